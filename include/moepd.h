@@ -92,8 +92,10 @@ enum { MOE_PHASE_P = 0, MOE_PHASE_D = 1, MOE_NUM_PHASES = 2 };
  * h are quantized by the kernels: per 32 values of a row, the shared exponent
  * is floor(log2(max |v|)) - 8 (clamped to [-127, 127]; -127 for an all-zero
  * block) and each code is v / 2^exponent rounded to nearest even after
- * clamping to +-448.  H and I must be multiples of 128. */
-enum { MOE_DTYPE_F32 = 0, MOE_DTYPE_BF16 = 1, MOE_DTYPE_FP8 = 2 };
+ * clamping to +-448.  H and I must be multiples of 128.
+ * MOE_DTYPE_FP4 names MX FP4 matrices in the calls of moepd_mx4.h; contexts
+ * do not take it. */
+enum { MOE_DTYPE_F32 = 0, MOE_DTYPE_BF16 = 1, MOE_DTYPE_FP8 = 2, MOE_DTYPE_FP4 = 3 };
 
 /* Status codes. */
 enum {

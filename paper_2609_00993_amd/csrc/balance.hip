@@ -1,0 +1,439 @@
+// The router's load-balance loss, per-expert counts and gradient
+// (include/moepd_balance.h).
+//
+// Both directions read the logits once; what bounds them is that stream, or, for
+// small batches, the launches.  One wave takes a token at a time, its logits in
+// registers (expert lane + 64 i in slot i), with wave-wide maxima and sums in
+// cross-lane moves; lanes accumulate their own experts' probabilities, so the sum
+// over tokens crosses lanes only once per piece.
+//
+// Pieces: the tokens are cut into chunks of equal length, a workgroup each, and a
+// chunk is cut where sequences end.  Chunk c and sequence s meet at most once,
+// and as tokens ascend either c or s does, so c + s numbers the pieces without a
+// gap in order: a piece's sums go to slot c + s, at most chunks + S - 1 slots.
+// The second kernel adds each sequence's slots in chunk order, so the
+// results do not depend on scheduling, and its last workgroup adds the sequences'
+// losses.  Sequences of any length mix: the work is dealt by tokens.
+#include <math.h>
+
+#include <type_traits>
+
+#include "common.h"
+#include "kernels.h"
+#include "moepd_balance.h"
+
+namespace moepd {
+
+namespace {
+
+struct BalanceArgs {
+  const void* logits;
+  const uint8_t* mask;   // null: all live
+  const int32_t* seq;    // null: one sequence of all tokens
+  long long stride;
+  int S, T, E, k;
+  float coef;
+};
+
+__device__ __forceinline__ int seq_begin(const BalanceArgs& g, int s) {
+  if (!g.seq) return s <= 0 ? 0 : g.T;
+  const int v = g.seq[s];
+  return v < 0 ? 0 : v < g.T ? v : g.T;
+}
+
+// The first sequence that ends past token t (S if none does).
+__device__ __forceinline__ int seq_of(const BalanceArgs& g, int t) {
+  int lo = 0, hi = g.S;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (seq_begin(g, mid + 1) > t) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, ROW_MASK, 0xF, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v = dpp_add<0xB1, 0xF>(v);   // as wave_extremum_u32
+  v = dpp_add<0x4E, 0xF>(v);
+  v = dpp_add<0x124, 0xF>(v);
+  v = dpp_add<0x128, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);
+  v = dpp_add<0x143, 0xC>(v);
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float dpp_max(float v) {
+  const uint32_t low = 0xff800000u;  // minus infinity
+  return fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(low, __float_as_uint(v), CTRL, ROW_MASK, 0xF, false)));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  v = dpp_max<0xB1, 0xF>(v);
+  v = dpp_max<0x4E, 0xF>(v);
+  v = dpp_max<0x124, 0xF>(v);
+  v = dpp_max<0x128, 0xF>(v);
+  v = dpp_max<0x142, 0xA>(v);
+  v = dpp_max<0x143, 0xC>(v);
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+
+template <int EPL, bool BF16>
+__device__ __forceinline__ void load_logits(const BalanceArgs& g, int t, float (&x)[EPL]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const int e = lane + i * kWave;
+    const long long at = t * g.stride + e;
+    x[i] = -INFINITY;
+    if (e < g.E) {
+      if constexpr (BF16) x[i] = bf16_to_f32(static_cast<const uint16_t*>(g.logits)[at]);
+      else x[i] = static_cast<const float*>(g.logits)[at];
+    }
+  }
+}
+
+// Probabilities of a row in place; all zero where every logit is minus infinity,
+// NaN where one is NaN or plus infinity (the sum of the exponentials then is).
+template <int EPL>
+__device__ __forceinline__ void softmax(float (&x)[EPL]) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) m = fmaxf(m, x[i]);
+  m = wave_max(m);
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    // minus infinity against itself would be NaN: such a term is 0 (m, when NaN, is not equal to it)
+    x[i] = x[i] == -INFINITY ? 0.f : expf(x[i] - m);
+    s += x[i];
+  }
+  s = wave_sum(s);
+  const float inv = s == 0.f ? 0.f : 1.f / s;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) x[i] *= inv;
+}
+
+constexpr int kBalanceWaves = 4;
+
+// A slot: E sums of probabilities, E counts, the live tokens.
+__host__ __device__ inline long long slot_words(int E) { return 2LL * E + 1; }
+
+template <int EPL, bool BF16>
+__global__ __launch_bounds__(64 * kBalanceWaves) void balance_pieces_kernel(BalanceArgs g,
+                                                                            const int32_t* __restrict__ idx, int chunk,
+                                                                            uint32_t* __restrict__ slots,
+                                                                            int32_t* __restrict__ ticket) {
+  __shared__ float sums[kBalanceWaves][EPL * kWave];
+  __shared__ int counts[EPL * kWave];
+  __shared__ int live_of[kBalanceWaves];
+  if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = blockIdx.x;
+  const int begin = c * chunk, end = min(begin + chunk, g.T);
+  for (int s = seq_of(g, begin); s < g.S; ++s) {
+    const int lo = max(begin, seq_begin(g, s)), hi = min(end, seq_begin(g, s + 1));
+    if (lo >= end) break;
+    if (lo >= hi) continue;  // an empty sequence
+    for (int e = threadIdx.x; e < g.E; e += 64 * kBalanceWaves) counts[e] = 0;
+    __syncthreads();
+    float acc[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) acc[i] = 0.f;
+    int live = 0;
+    for (int t = lo + wave; t < hi; t += kBalanceWaves) {
+      if (g.mask && !g.mask[t]) continue;
+      ++live;
+      float p[EPL];
+      load_logits<EPL, BF16>(g, t, p);
+      if (lane < g.k) {
+        const int e = idx[(long long)t * g.k + lane];
+        if ((uint32_t)e < (uint32_t)g.E) atomicAdd(&counts[e], 1);
+      }
+      softmax<EPL>(p);
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) acc[i] += p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) sums[wave][lane + i * kWave] = acc[i];
+    if (lane == 0) live_of[wave] = live;
+    __syncthreads();
+    uint32_t* slot = slots + (long long)(c + s) * slot_words(g.E);
+    for (int e = threadIdx.x; e < g.E; e += 64 * kBalanceWaves) {
+      float v = sums[0][e];
+#pragma unroll
+      for (int w = 1; w < kBalanceWaves; ++w) v += sums[w][e];
+      slot[e] = __float_as_uint(v);
+      slot[g.E + e] = (uint32_t)counts[e];
+    }
+    if (threadIdx.x == 0) {
+      int n = 0;
+      for (int w = 0; w < kBalanceWaves; ++w) n += live_of[w];
+      slot[2 * g.E] = (uint32_t)n;
+    }
+    __syncthreads();  // the LDS is free for the next piece
+  }
+}
+
+// Workgroup (x, s): 64 experts of sequence s.  Its waves deal the sequence's slots
+// among them, and their sums meet in LDS in wave order.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceArgs g, int chunk,
+                                                                      const uint32_t* __restrict__ slots,
+                                                                      float* __restrict__ parts, int32_t* ticket,
+                                                                      float* __restrict__ loss,
+                                                                      int32_t* __restrict__ counts, int32_t* live) {
+  __shared__ float ps[kJoinWaves][kWave];
+  __shared__ int cs[kJoinWaves][kWave], ns[kJoinWaves];
+  __shared__ int last;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int eg = blockIdx.x, groups = gridDim.x;
+  const int s = blockIdx.y + gridDim.y * blockIdx.z;
+  if (s >= g.S) return;
+  const int e = eg * kWave + lane;
+  const int lo = seq_begin(g, s), hi = seq_begin(g, s + 1);
+  float p = 0.f;
+  int cnt = 0, n = 0;
+  if (lo < hi) {
+    const int c1 = (hi - 1) / chunk;
+    for (int c = lo / chunk + wave; c <= c1; c += kJoinWaves) {
+      const uint32_t* slot = slots + (long long)(c + s) * slot_words(g.E);
+      if (e < g.E) {
+        p += __uint_as_float(slot[e]);
+        cnt += (int)slot[g.E + e];
+      }
+      n += (int)slot[2 * g.E];
+    }
+  }
+  ps[wave][lane] = p;
+  cs[wave][lane] = cnt;
+  if (lane == 0) ns[wave] = n;
+  __syncthreads();
+  if (wave == 0) {
+    p = 0.f;
+    cnt = n = 0;
+#pragma unroll
+    for (int w = 0; w < kJoinWaves; ++w) {
+      p += ps[w][lane];
+      cnt += cs[w][lane];
+      n += ns[w];
+    }
+    if (e < g.E) counts[(long long)s * g.E + e] = cnt;
+    // f P = (E c / (k T_s)) (p / T_s); counts and lengths are exact in float32 up to 2^24
+    const float each = n ? 1.f / (float)n : 0.f;
+    const float f = (float)g.E * (float)cnt / ((float)g.k * (float)(n ? n : 1));
+    const float v = wave_sum(e < g.E && n ? f * (p * each) : 0.f);
+    if (lane == 0) {
+      __hip_atomic_store(&parts[(long long)s * groups + eg], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (eg == 0) __hip_atomic_store(&live[s], n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      // release this workgroup's results; the last to arrive acquires everyone's
+      last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == groups * g.S - 1;
+    }
+  }
+  __syncthreads();
+  if (!last) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  float sum = 0.f;
+  int alive = 0;
+  for (int i = threadIdx.x; i < groups * g.S; i += 64 * kJoinWaves)
+    sum += __hip_atomic_load(&parts[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int i = threadIdx.x; i < g.S; i += 64 * kJoinWaves)
+    alive += __hip_atomic_load(&live[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 0;
+  ps[wave][lane] = sum;
+  cs[wave][lane] = alive;
+  __syncthreads();
+  if (wave == 0) {
+    sum = 0.f;
+    alive = 0;
+#pragma unroll
+    for (int w = 0; w < kJoinWaves; ++w) {
+      sum += ps[w][lane];
+      alive += cs[w][lane];
+    }
+    sum = wave_sum(sum);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) alive += __shfl_xor(alive, off, kWave);
+    if (lane == 0) {
+      *loss = alive ? g.coef * (sum / (float)alive) : 0.f;
+      live[g.S] = alive;
+    }
+  }
+}
+
+// One wave takes a run of consecutive tokens, so that a sequence's f stays in its registers.
+template <int EPL, bool BF16>
+__global__ __launch_bounds__(64 * kBalanceWaves) void balance_backward_kernel(BalanceArgs g, int run,
+                                                                              const int32_t* __restrict__ counts,
+                                                                              const int32_t* __restrict__ live,
+                                                                              const float* __restrict__ grad,
+                                                                              void* dlogits, long long dstride,
+                                                                              bool accumulate) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long long first = ((long long)blockIdx.x * kBalanceWaves + wave) * run;
+  if (first >= g.T) return;
+  const int begin = (int)first, end = (int)(first + run < g.T ? first + run : g.T);
+  const int seqs = live[g.S];
+  const float scale = (grad ? *grad : 1.f) * g.coef;
+  int s = seq_of(g, begin);
+  int s_begin = s < g.S ? seq_begin(g, s) : g.T, s_end = s < g.S ? seq_begin(g, s + 1) : g.T;
+  float f[EPL], weight = 0.f;
+  auto enter = [&] {
+    const int n = s < g.S ? live[s] : 0;
+    weight = n > 0 && seqs > 0 ? scale / ((float)n * (float)seqs) : 0.f;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      const int e = lane + i * kWave;
+      f[i] = e < g.E && n > 0 ? (float)g.E * (float)counts[(long long)s * g.E + e] / ((float)g.k * (float)n) : 0.f;
+    }
+  };
+  enter();
+  for (int t = begin; t < end; ++t) {
+    if (t >= s_end && s < g.S) {
+      while (s < g.S && t >= s_end) {
+        ++s;
+        if (s < g.S) s_end = seq_begin(g, s + 1);
+      }
+      s_begin = s < g.S ? seq_begin(g, s) : g.T;
+      enter();
+    }
+    const bool on = s < g.S && t >= s_begin && (!g.mask || g.mask[t]);
+    if (!on && accumulate) continue;
+    float d[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) d[i] = 0.f;
+    if (on) {
+      load_logits<EPL, BF16>(g, t, d);
+      softmax<EPL>(d);
+      float dot = 0.f;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) dot = __builtin_fmaf(f[i], d[i], dot);
+      dot = wave_sum(dot);
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) d[i] = weight * (d[i] * (f[i] - dot));
+    }
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      const int e = lane + i * kWave;
+      if (e >= g.E) continue;
+      const long long at = t * dstride + e;
+      if constexpr (BF16) {
+        uint16_t* o = static_cast<uint16_t*>(dlogits) + at;
+        *o = f32_to_bf16(accumulate ? bf16_to_f32(*o) + d[i] : d[i]);
+      } else {
+        float* o = static_cast<float*>(dlogits) + at;
+        *o = accumulate ? *o + d[i] : d[i];
+      }
+    }
+  }
+}
+
+// Tokens of a chunk: enough chunks to fill the GPU a few times over, at most
+// 1024, and at least four tokens to a wave.
+int chunk_of(int T) {
+  const int most = 1024;
+  int c = (T + most - 1) / most;
+  return c < 4 * kBalanceWaves ? 4 * kBalanceWaves : c;
+}
+
+constexpr int kTicketBytes = 64;
+
+int64_t workspace_bytes(int T, int E, int S) {
+  const int chunk = chunk_of(T);
+  const int64_t slots = (T + chunk - 1) / chunk + (int64_t)S;
+  return kTicketBytes + slots * slot_words(E) * 4 + (int64_t)S * ((E + 63) / 64) * 4;
+}
+
+template <class F>
+hipError_t by_experts(int E, F&& f) {
+  if (E <= 64) f(std::integral_constant<int, 1>{});
+  else if (E <= 128) f(std::integral_constant<int, 2>{});
+  else if (E <= 256) f(std::integral_constant<int, 4>{});
+  else if (E <= 512) f(std::integral_constant<int, 8>{});
+  else f(std::integral_constant<int, 16>{});
+  return hipGetLastError();
+}
+
+bool valid(int32_t dtype, int64_t* stride, const int32_t* seq, int32_t S, int32_t T, int32_t E, int32_t k,
+           hipStream_t stream) {
+  if (!stream || (dtype != MOE_DTYPE_F32 && dtype != MOE_DTYPE_BF16)) return false;
+  if (T < 0 || T > (1 << 24) || E < 1 || E > kMaxExperts || k < 1 || k > kMaxTopK || k > E) return false;
+  if (S < 1 || S > 65536 || (!seq && S != 1) || (uintptr_t)seq % 4) return false;
+  if (*stride == 0) *stride = E;
+  return *stride >= E;
+}
+
+bool aligned(const void* p, int32_t dtype) { return (uintptr_t)p % (dtype == MOE_DTYPE_F32 ? 4 : 2) == 0; }
+
+}  // namespace
+}  // namespace moepd
+
+using namespace moepd;
+
+extern "C" {
+
+int moe_balance_workspace(int32_t T, int32_t E, int32_t S, int64_t* bytes) {
+  if (!bytes || T < 0 || T > (1 << 24) || E < 1 || E > kMaxExperts || S < 1 || S > 65536) return MOE_ERR_INVALID_ARG;
+  *bytes = workspace_bytes(T, E, S);
+  return MOE_OK;
+}
+
+int moe_balance_loss(const void* logits, int32_t logits_dtype, int64_t logits_stride, const int32_t* topk_idx,
+                     const uint8_t* token_mask, const int32_t* seq_offsets, int32_t S, int32_t T, int32_t E, int32_t k,
+                     float coef, float* loss, int32_t* counts, int32_t* live, void* workspace, int64_t ws_bytes,
+                     hipStream_t stream) {
+  if (!valid(logits_dtype, &logits_stride, seq_offsets, S, T, E, k, stream)) return MOE_ERR_INVALID_ARG;
+  if (!loss || !counts || !live || !workspace || (uintptr_t)workspace % 256 ||
+      ((uintptr_t)loss | (uintptr_t)counts | (uintptr_t)live | (uintptr_t)topk_idx) % 4)
+    return MOE_ERR_INVALID_ARG;
+  if (T > 0 && (!logits || !topk_idx || !aligned(logits, logits_dtype))) return MOE_ERR_INVALID_ARG;
+  if (ws_bytes < workspace_bytes(T, E, S)) return MOE_ERR_CAPACITY;
+  const BalanceArgs g{logits, token_mask, seq_offsets, logits_stride, S, T, E, k, coef};
+  const int chunk = chunk_of(T), chunks = T > 0 ? (T + chunk - 1) / chunk : 1, groups = (E + 63) / 64;
+  int32_t* ticket = static_cast<int32_t*>(workspace);
+  uint32_t* slots = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + kTicketBytes);
+  float* parts = reinterpret_cast<float*>(slots + ((T + chunk - 1) / chunk + (long long)S) * slot_words(E));
+  auto pieces = [&](auto epl) {
+    constexpr int EPL = decltype(epl)::value;
+    if (logits_dtype == MOE_DTYPE_BF16)
+      balance_pieces_kernel<EPL, true><<<chunks, 64 * kBalanceWaves, 0, stream>>>(g, topk_idx, chunk, slots, ticket);
+    else
+      balance_pieces_kernel<EPL, false><<<chunks, 64 * kBalanceWaves, 0, stream>>>(g, topk_idx, chunk, slots, ticket);
+  };
+  if (by_experts(E, pieces) != hipSuccess) return MOE_ERR_HIP;
+  const int y = S < 1024 ? S : 1024;
+  balance_join_kernel<<<dim3(groups, y, (S + y - 1) / y), 64 * kJoinWaves, 0, stream>>>(g, chunk, slots, parts, ticket,
+                                                                                      loss, counts, live);
+  return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+int moe_balance_loss_backward(const void* logits, int32_t logits_dtype, int64_t logits_stride,
+                              const uint8_t* token_mask, const int32_t* seq_offsets, int32_t S, int32_t T, int32_t E,
+                              int32_t k, float coef, const int32_t* counts, const int32_t* live, const float* grad,
+                              void* dlogits, int64_t dlogits_stride, int32_t accumulate, hipStream_t stream) {
+  if (!valid(logits_dtype, &logits_stride, seq_offsets, S, T, E, k, stream)) return MOE_ERR_INVALID_ARG;
+  if (dlogits_stride == 0) dlogits_stride = E;
+  if (dlogits_stride < E) return MOE_ERR_INVALID_ARG;
+  if (dlogits == logits && dlogits && (accumulate || dlogits_stride != logits_stride)) return MOE_ERR_INVALID_ARG;
+  if (T == 0) return MOE_OK;
+  if (!logits || !counts || !live || !dlogits || !aligned(logits, logits_dtype) || !aligned(dlogits, logits_dtype) ||
+      ((uintptr_t)counts | (uintptr_t)live | (uintptr_t)grad) % 4)
+    return MOE_ERR_INVALID_ARG;
+  const BalanceArgs g{logits, token_mask, seq_offsets, logits_stride, S, T, E, k, coef};
+  // 8192 waves or one token each
+  const int run = (T + 8191) / 8192;
+  const int blocks = (int)(((T + run - 1) / run + kBalanceWaves - 1) / kBalanceWaves);
+  auto go = [&](auto epl) {
+    constexpr int EPL = decltype(epl)::value;
+    if (logits_dtype == MOE_DTYPE_BF16)
+      balance_backward_kernel<EPL, true><<<blocks, 64 * kBalanceWaves, 0, stream>>>(g, run, counts, live, grad, dlogits,
+                                                                                   dlogits_stride, accumulate != 0);
+    else
+      balance_backward_kernel<EPL, false><<<blocks, 64 * kBalanceWaves, 0, stream>>>(g, run, counts, live, grad, dlogits,
+                                                                                    dlogits_stride, accumulate != 0);
+  };
+  return by_experts(E, go) == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+}  // extern "C"

@@ -191,6 +191,11 @@ hipError_t launch_ffn_mx(int regime, int gemm, const PhaseBuffers& b, const MxBu
                          int e_loc, int H, int I, int bm, int max_m_tiles, double m_tiles_hint, Beside beside,
                          YieldTo yield, hipStream_t s);
 
+// rows of x (float32 or bf16) -> an MX FP4 matrix (see moe_mx4_quantize).
+hipError_t launch_mx4_quantize(const void* x, bool bf16, long long x_stride, long long rows, int cols,
+                               const int32_t* row_index, const int32_t* row_count, uint8_t* codes, uint8_t* scales,
+                               hipStream_t s);
+
 int ffn_f32_bm();
 hipError_t launch_ffn_f32(int gemm, const PhaseBuffers& b, const void* w_gu, const void* w_dn, int e_loc, int H,
                           int I, int max_m_tiles, hipStream_t s);

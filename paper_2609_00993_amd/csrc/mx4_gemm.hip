@@ -1,0 +1,449 @@
+// Products of MX FP4 matrices, dense or with one weight matrix per run of rows
+// (include/moepd_mx4.h), on v_mfma_scale_f32_32x32x64_f8f6f4: 32 x 32 outputs
+// and 64 values of K per instruction, float32 accumulation, block scales
+// applied by the matrix core.  The weights are the first operand, so lane l ends
+// with one row of `a` (l % 32) and 16 of its columns, 8 q + 4 (l / 32) + (0..3).
+#include <type_traits>
+
+#include "kernels.h"
+#include "moepd_mx4.h"
+#include "mx4.h"
+#include "pipeline.h"
+#include "tiles.h"
+
+namespace moepd {
+
+typedef int32_t v8i32_mx4 __attribute__((ext_vector_type(8)));
+typedef float f32x16_mx4 __attribute__((ext_vector_type(16)));
+typedef float f32x4_mx4 __attribute__((ext_vector_type(4)));
+
+enum Mx4Out : int { kMx4F32 = 0, kMx4Bf16 = 1, kMx4Fp4 = 2 };
+
+struct Mx4Args {
+  const uint8_t* a;
+  const uint8_t* as;
+  const uint8_t* w;
+  const uint8_t* ws;
+  void* c;
+  uint8_t* cs;
+  const int32_t* offsets;  // null: one group of all rows
+  long long rows, ldc;
+  int groups;
+  int n;        // columns of the output; a group's weight rows are n, or 2 n with gate and up
+  int slices;   // K / 256
+  int n_tiles;  // column tiles, rounded up to a multiple of 8
+  bool vec;     // rows of c take whole vectors of four columns
+};
+
+namespace {
+
+struct Mx4Tile {
+  int group;
+  long long m0, m_end;  // rows
+  int nt;               // column tile
+};
+
+// Group g's rows, clamped into [0, rows].
+__device__ __forceinline__ void mx4_group_rows(const Mx4Args& g, int e, long long& lo, long long& hi) {
+  const long long a = g.offsets[e], b = g.offsets[e + 1];
+  lo = a < 0 ? 0 : a < g.rows ? a : g.rows;
+  hi = b < lo ? lo : b < g.rows ? b : g.rows;
+}
+
+// Tile L of the launch: groups in order, within a group of mt tiles of bm rows
+// column tile 8 q + L % 8 for each q, with all its row tiles in a row: workgroup
+// L runs on XCD L % 8, so the row tiles that read one weight panel share an L2 and
+// every XCD streams an eighth of every group's weights.  Each wave finds its tile from
+// the offsets: 64 groups at a time, a scan of their tile counts.  False past the last tile.
+__device__ __forceinline__ bool mx4_tile(const Mx4Args& g, long long L, int bm, Mx4Tile& t) {
+  const int per_m = g.n_tiles;
+  long long local = L, lo = 0, hi = g.rows;
+  int e = 0, mt_e = 0;
+  if (!g.offsets) {
+    mt_e = (int)((g.rows + bm - 1) / bm);
+    if (L >= (long long)mt_e * per_m) return false;
+  } else {
+    const int lane = lane_id();
+    const long long want = L / per_m;  // row tiles before this one, over all groups
+    long long base = 0;
+    bool found = false;
+    for (int g0 = 0; g0 < g.groups; g0 += kWave) {
+      long long l = 0, h = 0;
+      if (g0 + lane < g.groups) mx4_group_rows(g, g0 + lane, l, h);
+      const int mt = (int)((h - l + bm - 1) / bm);
+      const int incl = wave_inclusive_scan(mt);
+      const uint64_t past = __ballot(base + incl > want);
+      if (past) {
+        const int src = __builtin_ctzll(past);
+        e = g0 + src;
+        mt_e = __builtin_amdgcn_readlane(mt, src);
+        local = L - (base + __builtin_amdgcn_readlane(incl, src) - mt_e) * per_m;
+        found = true;
+        break;
+      }
+      base += __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (!found) return false;
+    mx4_group_rows(g, e, lo, hi);
+  }
+  const int j = (int)(local >> 3);
+  const int q = j / mt_e, mt = j - q * mt_e;
+  t.group = e;
+  t.nt = 8 * q + (int)(local & 7);
+  t.m0 = lo + (long long)mt * bm;
+  t.m_end = t.m0 + bm < hi ? t.m0 + bm : hi;
+  return true;
+}
+
+__device__ __forceinline__ v8i32_mx4 widen(const u32x4& a) {
+  return v8i32_mx4{(int32_t)a[0], (int32_t)a[1], (int32_t)a[2], (int32_t)a[3], 0, 0, 0, 0};
+}
+
+// Step S (64 of a slice's 256 values): both operands' scale words hold the four
+// steps' scales, of which the instruction picks byte S.
+template <int S>
+__device__ __forceinline__ f32x16_mx4 mx4_mfma(const u32x4& w, const u32x4& a, const f32x16_mx4& acc, uint32_t sw,
+                                               uint32_t sa) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(w), widen(a), acc, 4, 4, S, (int)sw, S, (int)sa);
+}
+
+// silu(g) * u.  exp(-g) as 2^(t + lo): the product's rounding error and log2 e's
+// own, lo, would otherwise cost |g| ulp; with it, and the hardware's 2^x and
+// reciprocal (1 ulp each), the result is within a few ulp.
+__device__ __forceinline__ float mx4_silu_mul(float g, float u) {
+  constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
+  const float t = -g * kLog2e;
+  const float lo = __builtin_fmaf(-g, kLog2e, -t) + -g * kLog2eLow;
+  const float e = __builtin_amdgcn_exp2f(t);
+  const float ex = t < 128.f ? __builtin_fmaf(e, lo * kLn2, e) : e;
+  return g * __builtin_amdgcn_rcpf(1.f + ex) * u;
+}
+
+// Store one 32 x 32 block: lane (r, h) holds v[4 q + t] = column col0 + 8 q + 4 h + t of `row`.
+// The lanes of a row's two halves both call this (fp4 exchanges between them).
+template <int OUT>
+__device__ __forceinline__ void mx4_store(const Mx4Args& g, const float (&v)[16], long long row, bool live, int col0,
+                                          int h) {
+  if constexpr (OUT == kMx4Fp4) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
+      m = b > m ? b : m;
+    }
+    const uint32_t o = (uint32_t)__shfl_xor((int)m, 32, kWave);
+    m = o > m ? o : m;
+    const uint32_t byte = mx4_scale_byte(m);
+    const uint32_t w0 = mx4_codes8({v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, byte);
+    const uint32_t w1 = mx4_codes8({v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15]}, byte);
+    // this half's codes of quarter q are 16 bits; a quarter's word is (half 0, half 1)
+    const uint32_t p0 = (uint32_t)__shfl_xor((int)w0, 32, kWave), p1 = (uint32_t)__shfl_xor((int)w1, 32, kWave);
+    if (live && h == 0) {
+      const int blocks = (g.n + kMx4Slice - 1) / kMx4Slice * 8;
+      const long long rb = row >> 5;
+      const int r = (int)(row & 31), b = col0 >> 5;
+      store16(static_cast<uint8_t*>(g.c) + ((rb * blocks + b) * 32 + r) * 16,
+              u32x4{(w0 & 0xffffu) | (p0 << 16), (w0 >> 16) | (p0 & 0xffff0000u), (w1 & 0xffffu) | (p1 << 16),
+                    (w1 >> 16) | (p1 & 0xffff0000u)});
+      g.cs[(rb * (blocks / 8) + (b >> 3)) * kMx4SliceScales + ((b & 1) * 32 + r) * 4 + ((b & 7) >> 1)] = (uint8_t)byte;
+    }
+  } else {
+    if (!live) return;
+    const long long at = row * g.ldc + col0 + 4 * h;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int col = col0 + 4 * h + 8 * q;
+      if (g.vec && col + 4 <= g.n) {
+        if constexpr (OUT == kMx4F32) {
+          *reinterpret_cast<f32x4_mx4*>(static_cast<float*>(g.c) + at + 8 * q) =
+              f32x4_mx4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        } else {
+          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+          *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(g.c) + at + 8 * q) =
+              u32x2{(uint32_t)f32_to_bf16(v[4 * q]) | ((uint32_t)f32_to_bf16(v[4 * q + 1]) << 16),
+                    (uint32_t)f32_to_bf16(v[4 * q + 2]) | ((uint32_t)f32_to_bf16(v[4 * q + 3]) << 16)};
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (col + t < g.n) {
+            if constexpr (OUT == kMx4F32) static_cast<float*>(g.c)[at + 8 * q + t] = v[4 * q + t];
+            else static_cast<uint16_t*>(g.c)[at + 8 * q + t] = f32_to_bf16(v[4 * q + t]);
+          }
+      }
+    }
+  }
+}
+
+// A lane's place in a run of rows of a held matrix: its code bytes and scale bytes
+// from the block of the run's first row, or past every resource where the row does
+// not count (such loads give zeros and touch no memory).
+struct Mx4Lane {
+  int codes, scales;
+};
+constexpr int kMx4Nowhere = 0x7fffff00;
+__device__ __forceinline__ Mx4Lane mx4_lane(long long first, int row, bool counts, int slices, int h) {
+  const int rr = (int)(first & 31) + row;
+  const int b = rr >> 5, r = rr & 31;
+  return counts ? Mx4Lane{b * slices * kMx4SliceBytes + h * 512 + r * 16, b * slices * kMx4SliceScales + (h * 32 + r) * 4}
+                : Mx4Lane{kMx4Nowhere, kMx4Nowhere};
+}
+// The resource of `rows` rows from `first` on, which starts at the block of the first.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx4_rsrc(const uint8_t* p, long long first, int rows, int slices,
+                                                           int unit) {
+  const int blocks = ((int)(first & 31) + rows + 31) >> 5;
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(p + (first >> 5) * slices * unit), (short)0, blocks * slices * unit,
+                                           kBufferRsrcWord3);
+}
+__device__ __forceinline__ u32x4 mx4_load(const __amdgpu_buffer_rsrc_t& rsrc, int lane_off, int off) {
+  typedef uint32_t raw4 __attribute__((vector_size(16)));
+  const raw4 v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane_off, off, 0);
+  return u32x4{v[0], v[1], v[2], v[3]};
+}
+
+// ------------------------------------------------------------------ streaming tile
+
+// Few rows per group: what bounds the product is the stream of weights.  A wave
+// takes up to 32 MB rows and two panels of 32 weight rows (gate and up, or 64
+// columns; one panel where there are few tiles), each slice of a panel 4 KB of
+// consecutive memory straight into registers, two slices in flight.  The waves of
+// a workgroup share a tile and deal its slices among them; their sums meet in
+// LDS and are added in wave order.
+template <int MB, int NB>
+struct Mx4Slice4 {
+  u32x4 w[NB][4], a[MB][4];
+  uint32_t sw[NB], sa[MB];
+};
+
+template <int MB, int NB, bool GATED, int OUT>
+__device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile& t, float* lds) {
+  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int KT = g.slices;
+  constexpr int BN = GATED ? 32 : 32 * NB;
+  const int n0 = __builtin_amdgcn_readfirstlane(t.nt) * BN;
+  const long long w_first = (long long)t.group * (GATED ? 2 : 1) * g.n + n0;
+  const int m_rows = (int)(t.m_end - t.m0);
+  const __amdgpu_buffer_rsrc_t a_rsrc = mx4_rsrc(g.a, t.m0, m_rows, KT, kMx4SliceBytes);
+  const __amdgpu_buffer_rsrc_t as_rsrc = mx4_rsrc(g.as, t.m0, m_rows, KT, kMx4SliceScales);
+  Mx4Lane al[MB], wl[NB];
+  __amdgpu_buffer_rsrc_t w_rsrc[NB], ws_rsrc[NB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) al[m] = mx4_lane(t.m0, 32 * m + r, 32 * m + r < m_rows, KT, h);
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const long long first = GATED ? w_first + (j ? g.n : 0) : w_first + 32 * j;
+    const int left = g.n - n0 - (GATED ? 0 : 32 * j);  // weight rows from the panel's first on
+    const int rows = left < 0 ? 0 : left < 32 ? left : 32;
+    wl[j] = mx4_lane(first, r, r < rows, KT, h);
+    w_rsrc[j] = mx4_rsrc(g.w, first, rows, KT, kMx4SliceBytes);
+    ws_rsrc[j] = mx4_rsrc(g.ws, first, rows, KT, kMx4SliceScales);
+  }
+
+  auto load = [&](Mx4Slice4<MB, NB>& s, int kt) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      s.sw[j] = __builtin_amdgcn_raw_buffer_load_b32(ws_rsrc[j], wl[j].scales, kt * kMx4SliceScales, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s.w[j][i] = mx4_load(w_rsrc[j], wl[j].codes, kt * kMx4SliceBytes + i * 1024);
+    }
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      s.sa[m] = __builtin_amdgcn_raw_buffer_load_b32(as_rsrc, al[m].scales, kt * kMx4SliceScales, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s.a[m][i] = mx4_load(a_rsrc, al[m].codes, kt * kMx4SliceBytes + i * 1024);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  f32x16_mx4 acc[MB][NB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[m][j][q] = 0.f;
+  auto multiply = [&](const Mx4Slice4<MB, NB>& s) {
+    weave_run<0, 4>([&](auto i) {
+      constexpr int S = decltype(i)::value;
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[m][j] = mx4_mfma<S>(s.w[j][S], s.a[m][S], acc[m][j], s.sw[j], s.sa[m]);
+    });
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  Mx4Slice4<MB, NB> s0, s1;
+  // This wave's slices: wave, wave + waves, ...; the loop's loads carry no condition.
+  const int n = (KT - wave + waves - 1) / waves;
+  int kt = wave;
+  load(s0, kt);
+  if (n == 1) {
+    multiply(s0);
+  } else {
+    load(s1, kt + waves);
+    int i = 0;
+    for (; i + 3 < n; i += 2, kt += 2 * waves) {
+      multiply(s0);
+      load(s0, kt + 2 * waves);
+      multiply(s1);
+      load(s1, kt + 3 * waves);
+    }
+    multiply(s0);
+    if (i + 2 < n) load(s0, kt + 2 * waves);
+    multiply(s1);
+    if (i + 2 < n) multiply(s0);
+  }
+
+  if (waves > 1) {
+    f32x4_mx4* sums = reinterpret_cast<f32x4_mx4*>(lds);
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          sums[((wave * MB + m) * NB + j) * 256 + q * 64 + lane] =
+              f32x4_mx4{acc[m][j][4 * q], acc[m][j][4 * q + 1], acc[m][j][4 * q + 2], acc[m][j][4 * q + 3]};
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          for (int w = 1; w < waves; ++w) {
+            const f32x4_mx4 o = sums[((w * MB + m) * NB + j) * 256 + q * 64 + lane];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[m][j][4 * q + i] += o[i];
+          }
+  }
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    const long long row = t.m0 + 32 * m + r;
+    const bool live = row < t.m_end;
+    float v[16];
+    if constexpr (GATED) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = mx4_silu_mul(acc[m][0][i], acc[m][NB - 1][i]);
+      mx4_store<OUT>(g, v, row, live, n0, h);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = acc[m][j][i];
+        mx4_store<OUT>(g, v, row, live, n0 + 32 * j, h);
+      }
+    }
+  }
+}
+
+constexpr int kStreamRows = 64;
+template <int NB, bool GATED, int OUT>
+__global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args g) {
+  extern __shared__ __align__(16) float lds[];
+  Mx4Tile t;
+  if (!mx4_tile(g, (long long)blockIdx.y * gridDim.x + blockIdx.x, kStreamRows, t)) return;
+  if (t.nt * (GATED ? 32 : 32 * NB) >= (OUT == kMx4Fp4 ? (g.n + kMx4Slice - 1) / kMx4Slice * kMx4Slice : g.n)) return;
+  if (t.m_end - t.m0 <= 32) mx4_stream_tile<1, NB, GATED, OUT>(g, t, lds);
+  else mx4_stream_tile<2, NB, GATED, OUT>(g, t, lds);
+}
+
+inline int up8(long long v) { return (int)((v + 7) / 8 * 8); }
+
+}  // namespace
+
+hipError_t launch_mx4_gemm(Mx4Args g, bool gated, int out, hipStream_t s) {
+  const long long width = out == kMx4Fp4 ? (g.n + kMx4Slice - 1) / kMx4Slice * kMx4Slice : g.n;
+  // row tiles: at most one that is not full for each group that has a row
+  const long long touched = g.groups < g.rows ? g.groups : g.rows;
+  auto tiles_of = [&](int bn) { return up8((width + bn - 1) / bn) * (g.rows / kStreamRows + touched); };
+  auto go = [&](auto kernel, int bn, int panels) {
+    g.n_tiles = up8((width + bn - 1) / bn);
+    const long long tiles = tiles_of(bn);
+    // enough waves to keep the memory busy: 8 to a CU
+    int waves = 1;
+    while (waves < 8 && tiles * waves < 8 * 256 && waves * 2 <= g.slices) waves *= 2;
+    const size_t lds = waves > 1 ? (size_t)waves * (kStreamRows / 32) * panels * 4096 : 0;
+    kernel<<<grid_of(tiles, 64 * waves), 64 * waves, lds, s>>>(g);
+    return hipGetLastError();
+  };
+  auto by_out = [&](auto nb, auto gate) {
+    constexpr int NB = decltype(nb)::value;
+    constexpr bool GATED = decltype(gate)::value;
+    constexpr int BN = GATED ? 32 : 32 * NB;
+    if constexpr (GATED) {
+      if (out == kMx4Fp4) return go(mx4_stream_kernel<NB, GATED, kMx4Fp4>, BN, NB);
+    }
+    if (out == kMx4Bf16) return go(mx4_stream_kernel<NB, GATED, kMx4Bf16>, BN, NB);
+    return go(mx4_stream_kernel<NB, GATED, kMx4F32>, BN, NB);
+  };
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  if (gated) return by_out(Two{}, std::true_type{});
+  if (tiles_of(64) < 256) return by_out(One{}, std::false_type{});
+  return by_out(Two{}, std::false_type{});
+}
+
+}  // namespace moepd
+
+using namespace moepd;
+
+namespace {
+
+bool aligned(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
+
+int product(const uint8_t* a, const uint8_t* a_scales, int64_t rows, const uint8_t* w, const uint8_t* w_scales,
+            int32_t groups, const int32_t* offsets, int32_t n, int32_t k, void* out, uint8_t* out_scales,
+            int32_t out_dtype, int64_t out_stride, bool gated, hipStream_t stream) {
+  if (!stream || rows < 0 || rows > (1LL << 31) - 32 || n < 1 || n > MOE_MX4_MAX_COLS || k < 1 || k > MOE_MX4_MAX_COLS ||
+      groups < 1 || groups > MOE_MX4_MAX_GROUPS || (!offsets && groups != 1))
+    return MOE_ERR_INVALID_ARG;
+  const bool fp4 = gated && out_dtype == MOE_DTYPE_FP4;
+  if (!fp4 && out_dtype != MOE_DTYPE_F32 && out_dtype != MOE_DTYPE_BF16) return MOE_ERR_INVALID_ARG;
+  if (fp4 ? (n % 32 != 0 || out_stride != 0) : out_scales != nullptr) return MOE_ERR_INVALID_ARG;
+  if (out_stride == 0) out_stride = n;
+  if (out_stride < n) return MOE_ERR_INVALID_ARG;
+  if (rows == 0) return MOE_OK;
+  const int esz = out_dtype == MOE_DTYPE_F32 ? 4 : 2;
+  if (!a || !a_scales || !w || !w_scales || !out || (fp4 && !out_scales)) return MOE_ERR_INVALID_ARG;
+  if (!aligned(a, 16) || !aligned(a_scales, 16) || !aligned(w, 16) || !aligned(w_scales, 16) || !aligned(offsets, 4) ||
+      !aligned(out, fp4 ? 16 : esz) || !aligned(out_scales, 16))
+    return MOE_ERR_INVALID_ARG;
+  Mx4Args g{};
+  g.a = a;
+  g.as = a_scales;
+  g.w = w;
+  g.ws = w_scales;
+  g.c = out;
+  g.cs = out_scales;
+  g.offsets = offsets;
+  g.rows = rows;
+  g.ldc = out_stride;
+  g.groups = groups;
+  g.n = n;
+  g.slices = mx4_slices(k);
+  g.vec = aligned(out, 4 * esz) && out_stride % 4 == 0;
+  const int kind = fp4 ? kMx4Fp4 : out_dtype == MOE_DTYPE_BF16 ? kMx4Bf16 : kMx4F32;
+  return launch_mx4_gemm(g, gated, kind, stream) == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_mx4_gemm(const uint8_t* a, const uint8_t* a_scales, int64_t rows, const uint8_t* w, const uint8_t* w_scales,
+                 int32_t groups, const int32_t* offsets, int32_t n, int32_t k, void* out, int32_t out_dtype,
+                 int64_t out_stride, hipStream_t stream) {
+  return product(a, a_scales, rows, w, w_scales, groups, offsets, n, k, out, nullptr, out_dtype, out_stride, false,
+                 stream);
+}
+
+int moe_mx4_gemm_swiglu(const uint8_t* a, const uint8_t* a_scales, int64_t rows, const uint8_t* w,
+                        const uint8_t* w_scales, int32_t groups, const int32_t* offsets, int32_t n, int32_t k,
+                        void* out, uint8_t* out_scales, int32_t out_dtype, int64_t out_stride, hipStream_t stream) {
+  return product(a, a_scales, rows, w, w_scales, groups, offsets, n, k, out, out_scales, out_dtype, out_stride, true,
+                 stream);
+}
+
+}  // extern "C"

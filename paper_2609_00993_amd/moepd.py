@@ -1,5 +1,5 @@
-"""Thin ctypes binding of libmoepd (the C ABI declared in include/moepd.h and
-include/moepd_turnstile.h).
+"""Thin ctypes binding of libmoepd (the C ABI declared in include/moepd.h,
+include/moepd_mx4.h, include/moepd_balance.h and include/moepd_turnstile.h).
 
 Argument marshalling only: every step of the layer runs in the HIP library.
 Device buffers may be passed as integers (device addresses) or as objects
@@ -17,13 +17,13 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_char_p, c_double, c_int, c_int32, c_int64, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_void_p
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libmoepd.so")
 
 MOE_PHASE_P, MOE_PHASE_D, MOE_NUM_PHASES = 0, 1, 2
-MOE_DTYPE_F32, MOE_DTYPE_BF16, MOE_DTYPE_FP8 = 0, 1, 2
+MOE_DTYPE_F32, MOE_DTYPE_BF16, MOE_DTYPE_FP8, MOE_DTYPE_FP4 = 0, 1, 2, 3
 
 MOE_OK = 0
 MOE_ERR_INVALID_ARG = -1
@@ -145,6 +145,21 @@ _SIGNATURES = {
     "moe_timing_read": (c_int, [c_void_p, c_int, c_int, POINTER(c_double), POINTER(c_int32)]),
     "moe_kernel_name": (c_char_p, [c_int]),
     "moe_clock_probe": (c_int, [c_void_p, c_int32, c_void_p]),
+    "moe_mx4_size": (c_int, [c_int64, c_int32, POINTER(c_int64), POINTER(c_int64)]),
+    "moe_mx4_quantize": (c_int, [c_void_p, c_int32, c_int64, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                 c_void_p]),
+    "moe_mx4_pack": (c_int, [c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p]),
+    "moe_mx4_dequantize": (c_int, [c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_int32, c_int64, c_void_p]),
+    "moe_mx4_gemm": (c_int, [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int32, c_void_p, c_int32, c_int32,
+                             c_void_p, c_int32, c_int64, c_void_p]),
+    "moe_mx4_gemm_swiglu": (c_int, [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int32, c_void_p, c_int32,
+                                    c_int32, c_void_p, c_void_p, c_int32, c_int64, c_void_p]),
+    "moe_balance_workspace": (c_int, [c_int32, c_int32, c_int32, POINTER(c_int64)]),
+    "moe_balance_loss": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32,
+                                 c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]),
+    "moe_balance_loss_backward": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_int32, c_int32, c_int32,
+                                          c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int32,
+                                          c_void_p]),
     "moe_turnstile_create": (c_int, [c_int32, c_int32, POINTER(c_void_p)]),
     "moe_turnstile_destroy": (c_int, [c_void_p]),
     "moe_turnstile_set_span": (c_int, [c_void_p, c_int32]),
@@ -308,6 +323,68 @@ def moe_kernel_name(kernel: int) -> str:
 def moe_clock_probe(stream, spin_us: int, out_dev) -> int:
     """out_dev: device buffer of two uint64 (shader-clock ticks, 100 MHz ticks)."""
     return _lib.moe_clock_probe(_stream(stream), spin_us, _ptr(out_dev))
+
+
+# ---- MX FP4 matrices and products (include/moepd_mx4.h) ----
+
+
+def moe_mx4_size(rows: int, cols: int):
+    """(status, code bytes, scale bytes)"""
+    codes, scales = c_int64(), c_int64()
+    st = _lib.moe_mx4_size(rows, cols, byref(codes), byref(scales))
+    return st, codes.value, scales.value
+
+
+def moe_mx4_quantize(x, x_dtype: int, x_stride: int, rows: int, cols: int, row_index, row_count, codes, scales,
+                     stream) -> int:
+    return _lib.moe_mx4_quantize(_ptr(x), x_dtype, x_stride, rows, cols, _ptr(row_index), _ptr(row_count), _ptr(codes),
+                                 _ptr(scales), _stream(stream))
+
+
+def moe_mx4_pack(in_codes, in_scales, rows: int, cols: int, codes, scales, stream) -> int:
+    return _lib.moe_mx4_pack(_ptr(in_codes), _ptr(in_scales), rows, cols, _ptr(codes), _ptr(scales), _stream(stream))
+
+
+def moe_mx4_dequantize(codes, scales, rows: int, cols: int, out, out_dtype: int, out_stride: int, stream) -> int:
+    return _lib.moe_mx4_dequantize(_ptr(codes), _ptr(scales), rows, cols, _ptr(out), out_dtype, out_stride,
+                                   _stream(stream))
+
+
+def moe_mx4_gemm(a, a_scales, rows: int, w, w_scales, groups: int, offsets, n: int, k: int, out, out_dtype: int,
+                 out_stride: int, stream) -> int:
+    return _lib.moe_mx4_gemm(_ptr(a), _ptr(a_scales), rows, _ptr(w), _ptr(w_scales), groups, _ptr(offsets), n, k,
+                             _ptr(out), out_dtype, out_stride, _stream(stream))
+
+
+def moe_mx4_gemm_swiglu(a, a_scales, rows: int, w, w_scales, groups: int, offsets, n: int, k: int, out, out_scales,
+                        out_dtype: int, out_stride: int, stream) -> int:
+    return _lib.moe_mx4_gemm_swiglu(_ptr(a), _ptr(a_scales), rows, _ptr(w), _ptr(w_scales), groups, _ptr(offsets), n, k,
+                                    _ptr(out), _ptr(out_scales), out_dtype, out_stride, _stream(stream))
+
+
+# ---- the router's balance loss (include/moepd_balance.h) ----
+
+
+def moe_balance_workspace(T: int, E: int, S: int):
+    """(status, bytes)"""
+    n = c_int64()
+    st = _lib.moe_balance_workspace(T, E, S, byref(n))
+    return st, n.value
+
+
+def moe_balance_loss(logits, logits_dtype: int, logits_stride: int, topk_idx, token_mask, seq_offsets, S: int, T: int,
+                     E: int, k: int, coef: float, loss, counts, live, workspace, workspace_bytes: int, stream) -> int:
+    return _lib.moe_balance_loss(_ptr(logits), logits_dtype, logits_stride, _ptr(topk_idx), _ptr(token_mask),
+                                 _ptr(seq_offsets), S, T, E, k, coef, _ptr(loss), _ptr(counts), _ptr(live),
+                                 _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def moe_balance_loss_backward(logits, logits_dtype: int, logits_stride: int, token_mask, seq_offsets, S: int, T: int,
+                              E: int, k: int, coef: float, counts, live, grad, dlogits, dlogits_stride: int,
+                              accumulate: bool, stream) -> int:
+    return _lib.moe_balance_loss_backward(_ptr(logits), logits_dtype, logits_stride, _ptr(token_mask),
+                                          _ptr(seq_offsets), S, T, E, k, coef, _ptr(counts), _ptr(live), _ptr(grad),
+                                          _ptr(dlogits), dlogits_stride, int(bool(accumulate)), _stream(stream))
 
 
 # ---- turnstile (include/moepd_turnstile.h) ----
