@@ -50,21 +50,50 @@ __device__ __forceinline__ void mx4_group_rows(const Mx4Args& g, int e, long lon
   hi = b < lo ? lo : b < g.rows ? b : g.rows;
 }
 
-// Tile L of the launch: groups in order, within a group of mt tiles of bm rows
-// column tile 8 q + L % 8 for each q, with all its row tiles in a row: workgroup
-// L runs on XCD L % 8, so the row tiles that read one weight panel share an L2 and
-// every XCD streams an eighth of every group's weights.  Each wave finds its tile from
-// the offsets: 64 groups at a time, a scan of their tile counts.  False past the last tile.
-__device__ __forceinline__ bool mx4_tile(const Mx4Args& g, long long L, int bm, Mx4Tile& t) {
-  const int per_m = g.n_tiles;
-  long long local = L, lo = 0, hi = g.rows;
+// The tile of workgroup b, if any, found by each wave from the offsets: 64 groups
+// at a time, a scan of their counts of row tiles of at most bm rows.
+//
+// STRIPED (streaming tiles): groups in order, within a group of mt row tiles column
+// tile 8 q + b % 8 for each q, with all its row tiles in a row: workgroup b runs on
+// XCD b % 8, so the row tiles that read one weight panel share an L2, and every XCD
+// streams an eighth of every group's weights.
+//
+// Otherwise (ring tiles): a group's rows are shared evenly among its row tiles; its
+// tiles run over blocks of four column tiles, in each row tile by row tile; and runs of
+// 32 consecutive tiles (8 row x 4 column tiles, the workgroups that one XCD's 32 CUs
+// hold at a time) are dealt to the XCDs in turn, so that an XCD's L2 serves each row
+// block to four workgroups and each weight panel to eight.  The last runs, when
+// they do not go round, are dealt tile by tile.
+template <bool STRIPED>
+__device__ __forceinline__ bool mx4_tile(const Mx4Args& g, long long b, int bm, Mx4Tile& t) {
+  const int lane = lane_id();
+  long long lo = 0, hi = g.rows, local;
   int e = 0, mt_e = 0;
+  // row tiles of all groups
+  long long m_total = 0;
   if (!g.offsets) {
-    mt_e = (int)((g.rows + bm - 1) / bm);
-    if (L >= (long long)mt_e * per_m) return false;
+    m_total = (g.rows + bm - 1) / bm;
+  } else if (!STRIPED) {
+    for (int g0 = 0; g0 < g.groups; g0 += kWave) {
+      long long l = 0, h = 0;
+      if (g0 + lane < g.groups) mx4_group_rows(g, g0 + lane, l, h);
+      m_total += __builtin_amdgcn_readlane(wave_inclusive_scan((int)((h - l + bm - 1) / bm)), 63);
+    }
+  }
+  long long L = b;
+  if constexpr (!STRIPED) {
+    const long long total = m_total * g.n_tiles;
+    const int x = (int)(b & 7);
+    const long long slot = b >> 3, base = slot / kXcdGroup * (8 * kXcdGroup), j = slot % kXcdGroup;
+    L = base + 8 * kXcdGroup <= total ? base + x * kXcdGroup + j : base + 8 * j + x;
+    if (L >= total) return false;
+  }
+  if (!g.offsets) {
+    if (L >= m_total * g.n_tiles) return false;
+    local = L;
+    mt_e = (int)m_total;
   } else {
-    const int lane = lane_id();
-    const long long want = L / per_m;  // row tiles before this one, over all groups
+    const long long want = L / g.n_tiles;  // row tiles before this one, over all groups
     long long base = 0;
     bool found = false;
     for (int g0 = 0; g0 < g.groups; g0 += kWave) {
@@ -77,7 +106,7 @@ __device__ __forceinline__ bool mx4_tile(const Mx4Args& g, long long L, int bm, 
         const int src = __builtin_ctzll(past);
         e = g0 + src;
         mt_e = __builtin_amdgcn_readlane(mt, src);
-        local = L - (base + __builtin_amdgcn_readlane(incl, src) - mt_e) * per_m;
+        local = L - (base + __builtin_amdgcn_readlane(incl, src) - mt_e) * g.n_tiles;
         found = true;
         break;
       }
@@ -86,12 +115,22 @@ __device__ __forceinline__ bool mx4_tile(const Mx4Args& g, long long L, int bm, 
     if (!found) return false;
     mx4_group_rows(g, e, lo, hi);
   }
-  const int j = (int)(local >> 3);
-  const int q = j / mt_e, mt = j - q * mt_e;
   t.group = e;
-  t.nt = 8 * q + (int)(local & 7);
-  t.m0 = lo + (long long)mt * bm;
-  t.m_end = t.m0 + bm < hi ? t.m0 + bm : hi;
+  const int at = (int)local;
+  if constexpr (STRIPED) {
+    const int j = at >> 3, q = j / mt_e;
+    t.nt = 8 * q + (at & 7);
+    t.m0 = lo + (long long)(j - q * mt_e) * bm;
+    t.m_end = t.m0 + bm < hi ? t.m0 + bm : hi;
+  } else {
+    const int q = at / (4 * mt_e), r = at - q * 4 * mt_e;
+    const int width = g.n_tiles - 4 * q < 4 ? g.n_tiles - 4 * q : 4;
+    const int mt = r / width;
+    t.nt = 4 * q + r - mt * width;
+    const int per = (int)((hi - lo + mt_e - 1) / mt_e);
+    t.m0 = lo + (long long)mt * per;
+    t.m_end = t.m0 + per < hi ? t.m0 + per : hi;
+  }
   return true;
 }
 
@@ -189,9 +228,11 @@ __device__ __forceinline__ Mx4Lane mx4_lane(long long first, int row, bool count
                 : Mx4Lane{kMx4Nowhere, kMx4Nowhere};
 }
 // The resource of `rows` rows from `first` on, which starts at the block of the first.
+// At least one block (of which no lane reads anything where there is no row), so that
+// every slice's offset lies within it.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t mx4_rsrc(const uint8_t* p, long long first, int rows, int slices,
                                                            int unit) {
-  const int blocks = ((int)(first & 31) + rows + 31) >> 5;
+  const int blocks = rows > 0 ? ((int)(first & 31) + rows + 31) >> 5 : 1;
   return __builtin_amdgcn_make_buffer_rsrc((void*)(p + (first >> 5) * slices * unit), (short)0, blocks * slices * unit,
                                            kBufferRsrcWord3);
 }
@@ -343,10 +384,217 @@ template <int NB, bool GATED, int OUT>
 __global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args g) {
   extern __shared__ __align__(16) float lds[];
   Mx4Tile t;
-  if (!mx4_tile(g, (long long)blockIdx.y * gridDim.x + blockIdx.x, kStreamRows, t)) return;
+  if (!mx4_tile<true>(g, (long long)blockIdx.y * gridDim.x + blockIdx.x, kStreamRows, t)) return;
   if (t.nt * (GATED ? 32 : 32 * NB) >= (OUT == kMx4Fp4 ? (g.n + kMx4Slice - 1) / kMx4Slice * kMx4Slice : g.n)) return;
   if (t.m_end - t.m0 <= 32) mx4_stream_tile<1, NB, GATED, OUT>(g, t, lds);
   else mx4_stream_tile<2, NB, GATED, OUT>(g, t, lds);
+}
+
+// ------------------------------------------------------------------ ring tile
+
+// Many rows per group: four waves side by side along the weights.  Each wave
+// takes all 32 MB rows of the tile and two panels of 32 weight rows (gate and
+// up, or 64 columns).  No two waves use the same weights, so these go straight
+// into registers; the rows of `a`, which all four read, travel by DMA into a
+// ring of SA slots of one slice (256 values) each, where one operand of one MFMA is
+// 1 KB in a row.  With 256 rows that is, for the 512 cycles of a step's 16
+// MFMAs per SIMD, 32 KB of LDS reads (half the LDS's rate) and 16 KB from L2.
+//
+// A slice is four steps of 64 values.  Step s multiplies while the next step's
+// operands come from LDS; the registers of its weights are then free, and the
+// weights of step s two slices on are requested into them during step s + 1 (those of
+// step 3, and the scales, during the next slice's step 0).  The slice's barrier
+// stands before step 3, when every wave holds the last operands of the slice: its
+// slot is free for slice kt + SA, and slice kt + 1, which each wave has waited for,
+// is complete.  Requests past the last slice carry a lane offset outside
+// the resource: they move no memory, and every slice has the same instructions, so the
+// counted waits are exact throughout.
+template <int MB, int SA, bool GATED, int OUT>
+__device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t, u32x4* lds) {
+  constexpr int kSlot = MB * 256;  // 16-byte units
+  static_assert(SA >= 3, "the wait below counts whole slices between a slot's request and its use");
+  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int KT = g.slices;
+  const int n0 = __builtin_amdgcn_readfirstlane(t.nt) * (GATED ? 128 : 256) + wave * (GATED ? 32 : 64);
+  const int group = __builtin_amdgcn_readfirstlane(t.group);
+  const long long m0 = t.m0;
+  const int m_rows = __builtin_amdgcn_readfirstlane((int)(t.m_end - t.m0));
+  const __amdgpu_buffer_rsrc_t a_rsrc = mx4_rsrc(g.a, m0, m_rows, KT, kMx4SliceBytes);
+  const __amdgpu_buffer_rsrc_t as_rsrc = mx4_rsrc(g.as, m0, m_rows, KT, kMx4SliceScales);
+  __amdgpu_buffer_rsrc_t w_rsrc[2], ws_rsrc[2];
+  // Row block b is MB - 1 blocks at most past the first; only the last one may be cut short.
+  const Mx4Lane full = mx4_lane(m0, r, true, KT, h), cut = mx4_lane(m0, r, 32 * (MB - 1) + r < m_rows, KT, h);
+  Mx4Lane wl[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const long long first = (long long)group * (GATED ? 2 : 1) * g.n + n0 + (GATED ? j * g.n : 32 * j);
+    const int left = g.n - n0 - (GATED ? 0 : 32 * j);
+    const int rows = left < 0 ? 0 : left < 32 ? left : 32;
+    wl[j] = mx4_lane(first, r, r < rows, KT, h);
+    w_rsrc[j] = mx4_rsrc(g.w, first, rows, KT, kMx4SliceBytes);
+    ws_rsrc[j] = mx4_rsrc(g.ws, first, rows, KT, kMx4SliceScales);
+  }
+
+  u32x4 wf[2][2][4];  // [slice parity][panel][step]
+  uint32_t sw[2][2], sa[2][MB];
+  u32x4 af[2][MB];  // [step parity]
+  f32x16_mx4 acc[MB][2];
+
+  // Requests name slice kt; past the last one the lanes read nowhere, at the last one's place.
+  int w_at, full_codes, cut_codes, full_scales, cut_scales, wc[2], wsc[2];
+  auto aim_w = [&](int kt) {
+    w_at = kt < KT ? kt : KT - 1;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      wc[j] = kt < KT ? wl[j].codes : kMx4Nowhere;
+      wsc[j] = kt < KT ? wl[j].scales : kMx4Nowhere;
+    }
+    full_scales = kt < KT ? full.scales : kMx4Nowhere;
+    cut_scales = kt < KT ? cut.scales : kMx4Nowhere;
+  };
+  int a_at;
+  auto aim_a = [&](int kt) {
+    a_at = kt < KT ? kt : KT - 1;
+    full_codes = kt < KT ? full.codes : kMx4Nowhere;
+    cut_codes = kt < KT ? cut.codes : kMx4Nowhere;
+  };
+  // Row block b of `a`, of which this wave moves step `wave`.  The lane offset carries all that
+  // depends on the row: it is the part that is checked against the resource.
+  auto request_a = [&](int b, int slot) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rsrc, MOEPD_LPTR(lds + slot * kSlot + (b * 4 + wave) * 64), 16,
+                                             (b == MB - 1 ? cut_codes : full_codes) + b * KT * kMx4SliceBytes,
+                                             a_at * kMx4SliceBytes + wave * 1024, 0, 0);
+  };
+  auto load_w = [&](int j, int s, int p) {
+    wf[p][j][s] = mx4_load(w_rsrc[j], wc[j], w_at * kMx4SliceBytes + s * 1024);
+  };
+  auto load_sw = [&](int j, int p) {
+    sw[p][j] = __builtin_amdgcn_raw_buffer_load_b32(ws_rsrc[j], wsc[j], w_at * kMx4SliceScales, 0);
+  };
+  auto load_sa = [&](int b, int p) {
+    sa[p][b] = __builtin_amdgcn_raw_buffer_load_b32(
+        as_rsrc, (b == MB - 1 ? cut_scales : full_scales) + b * KT * kMx4SliceScales, w_at * kMx4SliceScales, 0);
+  };
+
+  // In program order: the waits count requests.
+#pragma unroll
+  for (int st = 0; st < SA; ++st) {
+    aim_a(st);
+#pragma unroll
+    for (int b = 0; b < MB; ++b) request_a(b, st);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  aim_w(0);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) load_sw(j, 0);
+#pragma unroll
+  for (int b = 0; b < MB; ++b) load_sa(b, 0);
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) load_w(j, s, 0);
+  __builtin_amdgcn_sched_barrier(0);
+  aim_w(1);
+#pragma unroll
+  for (int s = 0; s < 3; ++s)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) load_w(j, s, 1);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[m][j][q] = 0.f;
+
+  constexpr int kPrologue = (SA - 1) * MB + 16 + MB;
+  wait_vmcnt_lgkm0<(kPrologue < 63 ? kPrologue : 63)>();
+  bare_barrier();
+#pragma unroll
+  for (int b = 0; b < MB; ++b) af[0][b] = lds[b * 256 + lane];
+
+  int slot = 0;
+  auto slice = [&](auto parity, int kt) {
+    constexpr int P = decltype(parity)::value, Q = P ^ 1;
+    const u32x4* here = lds + slot * kSlot + lane;
+    const int next = slot + 1 == SA ? 0 : slot + 1;
+    const u32x4* there = lds + next * kSlot + lane;
+    auto mul = [&](auto step) {
+      constexpr int S = decltype(step)::value;
+      return [&](auto i) {
+        constexpr int m = decltype(i)::value / 2, j = decltype(i)::value % 2;
+        acc[m][j] = mx4_mfma<S>(wf[P][j][S], af[S & 1][m], acc[m][j], sw[P][j], sa[P][m]);
+      };
+    };
+    using C0 = std::integral_constant<int, 0>;
+    using C1 = std::integral_constant<int, 1>;
+    using C2 = std::integral_constant<int, 2>;
+    using C3 = std::integral_constant<int, 3>;
+    weave<2 * MB, MB, 4 + MB>(mul(C0{}), [&](auto b) { af[1][b] = here[(b * 4 + 1) * 64]; },
+                              [&](auto i) {
+                                if constexpr (i < 2) load_w(i, 3, Q);
+                                else if constexpr (i < 4) load_sw(i - 2, Q);
+                                else load_sa(i - 4, Q);
+                              });
+    aim_w(kt + 2);
+    weave<2 * MB, MB, 2>(mul(C1{}), [&](auto b) { af[0][b] = here[(b * 4 + 2) * 64]; },
+                         [&](auto j) { load_w(j, 0, P); });
+    weave<2 * MB, MB, 2>(mul(C2{}), [&](auto b) { af[1][b] = here[(b * 4 + 3) * 64]; },
+                         [&](auto j) { load_w(j, 1, P); });
+    // requests younger than slice kt + 1 of `a`: all of SA - 2 slices and this one's so far
+    constexpr int kYounger = (SA - 2) * (10 + 2 * MB) + 8 + MB;
+    wait_vmcnt_lgkm0<(kYounger < 63 ? kYounger : 63)>();
+    bare_barrier();
+    aim_a(kt + SA);
+    weave<2 * MB, MB, 2 + MB>(mul(C3{}), [&](auto b) { af[0][b] = there[b * 256]; },
+                              [&](auto i) {
+                                if constexpr (i < 2) load_w(i, 2, P);
+                                else request_a(i - 2, slot);
+                              });
+    slot = next;
+  };
+  int kt = 0;
+  for (; kt + 1 < KT; kt += 2) {
+    slice(std::integral_constant<int, 0>{}, kt);
+    slice(std::integral_constant<int, 1>{}, kt + 1);
+  }
+  if (kt < KT) slice(std::integral_constant<int, 0>{}, kt);
+
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    const bool live = 32 * m + r < m_rows;
+    const long long row = m0 + 32 * m + r;
+    float v[16];
+    if constexpr (GATED) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = mx4_silu_mul(acc[m][0][i], acc[m][1][i]);
+      mx4_store<OUT>(g, v, row, live, n0, h);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = acc[m][j][i];
+        mx4_store<OUT>(g, v, row, live, n0 + 32 * j, h);
+      }
+    }
+  }
+}
+
+// Tiles of up to 32 MAXB rows, cut to the 32-row blocks that they hold.  Up to 128
+// rows two workgroups share a CU; up to 256, one takes it.
+constexpr int kRingSlots = 3;
+template <int MAXB, bool GATED, int OUT>
+__global__ __launch_bounds__(256, MAXB <= 4 ? 2 : 1) void mx4_ring_kernel(Mx4Args g) {
+  __shared__ u32x4 lds[kRingSlots * MAXB * 256];
+  Mx4Tile t;
+  if (!mx4_tile<false>(g, (long long)blockIdx.y * gridDim.x + blockIdx.x, 32 * MAXB, t)) return;
+  const int blocks = __builtin_amdgcn_readfirstlane((int)((t.m_end - t.m0 + 31) / 32));
+  if (blocks <= 0) return;  // fewer rows than tiles: an even share of none
+  weave_run<1, MAXB + 1>([&](auto mb) {
+    constexpr int MB = decltype(mb)::value;
+    if (blocks == MB) mx4_ring_tile<MB, kRingSlots, GATED, OUT>(g, t, lds);
+  });
 }
 
 inline int up8(long long v) { return (int)((v + 7) / 8 * 8); }
@@ -357,32 +605,38 @@ hipError_t launch_mx4_gemm(Mx4Args g, bool gated, int out, hipStream_t s) {
   const long long width = out == kMx4Fp4 ? (g.n + kMx4Slice - 1) / kMx4Slice * kMx4Slice : g.n;
   // row tiles: at most one that is not full for each group that has a row
   const long long touched = g.groups < g.rows ? g.groups : g.rows;
-  auto tiles_of = [&](int bn) { return up8((width + bn - 1) / bn) * (g.rows / kStreamRows + touched); };
-  auto go = [&](auto kernel, int bn, int panels) {
-    g.n_tiles = up8((width + bn - 1) / bn);
-    const long long tiles = tiles_of(bn);
+  const long long mean = g.rows / touched;
+  auto launch = [&](auto kernel, int bm, int bn, int threads, size_t lds, int round) {
+    g.n_tiles = (int)((width + bn - 1) / bn + round - 1) / round * round;
+    const long long tiles = (g.rows / bm + touched) * g.n_tiles;
+    // whole runs of 32 tiles to each XCD
+    const long long blocks = round == 8 ? tiles : (tiles + 8 * kXcdGroup - 1) / (8 * kXcdGroup) * (8 * kXcdGroup);
+    kernel<<<grid_of(blocks, threads), threads, lds, s>>>(g);
+    return hipGetLastError();
+  };
+  auto stream = [&](auto kernel, int bn, int panels) {
+    const long long tiles = up8((width + bn - 1) / bn) * (g.rows / kStreamRows + touched);
     // enough waves to keep the memory busy: 8 to a CU
     int waves = 1;
     while (waves < 8 && tiles * waves < 8 * 256 && waves * 2 <= g.slices) waves *= 2;
-    const size_t lds = waves > 1 ? (size_t)waves * (kStreamRows / 32) * panels * 4096 : 0;
-    kernel<<<grid_of(tiles, 64 * waves), 64 * waves, lds, s>>>(g);
-    return hipGetLastError();
+    return launch(kernel, kStreamRows, bn, 64 * waves, waves > 1 ? (size_t)waves * (kStreamRows / 32) * panels * 4096 : 0, 8);
   };
-  auto by_out = [&](auto nb, auto gate) {
-    constexpr int NB = decltype(nb)::value;
+  const bool few = up8((width + 63) / 64) * (g.rows / kStreamRows + touched) < 256;
+  auto go = [&](auto gate, auto kind) {
     constexpr bool GATED = decltype(gate)::value;
-    constexpr int BN = GATED ? 32 : 32 * NB;
-    if constexpr (GATED) {
-      if (out == kMx4Fp4) return go(mx4_stream_kernel<NB, GATED, kMx4Fp4>, BN, NB);
-    }
-    if (out == kMx4Bf16) return go(mx4_stream_kernel<NB, GATED, kMx4Bf16>, BN, NB);
-    return go(mx4_stream_kernel<NB, GATED, kMx4F32>, BN, NB);
+    constexpr int OUT = decltype(kind)::value;
+    if (mean >= 160) return launch(mx4_ring_kernel<8, GATED, OUT>, 256, GATED ? 128 : 256, 256, 0, 1);
+    if (mean >= 32) return launch(mx4_ring_kernel<4, GATED, OUT>, 128, GATED ? 128 : 256, 256, 0, 1);
+    if constexpr (GATED) return stream(mx4_stream_kernel<2, true, OUT>, 32, 2);
+    else return few ? stream(mx4_stream_kernel<1, false, OUT>, 32, 1) : stream(mx4_stream_kernel<2, false, OUT>, 64, 2);
   };
-  using One = std::integral_constant<int, 1>;
-  using Two = std::integral_constant<int, 2>;
-  if (gated) return by_out(Two{}, std::true_type{});
-  if (tiles_of(64) < 256) return by_out(One{}, std::false_type{});
-  return by_out(Two{}, std::false_type{});
+  using Plain = std::false_type;
+  using Gated = std::true_type;
+  using F32 = std::integral_constant<int, kMx4F32>;
+  using Bf16 = std::integral_constant<int, kMx4Bf16>;
+  using Fp4 = std::integral_constant<int, kMx4Fp4>;
+  if (gated) return out == kMx4Fp4 ? go(Gated{}, Fp4{}) : out == kMx4Bf16 ? go(Gated{}, Bf16{}) : go(Gated{}, F32{});
+  return out == kMx4Bf16 ? go(Plain{}, Bf16{}) : go(Plain{}, F32{});
 }
 
 }  // namespace moepd
