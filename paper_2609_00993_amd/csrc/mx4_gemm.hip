@@ -37,11 +37,16 @@ struct Mx4Args {
 
 namespace {
 
-struct Mx4Tile {
+struct Mx4Tile {  // wave-uniform
   int group;
   long long m0, m_end;  // rows
   int nt;               // column tile
 };
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ long long uniform(long long v) {
+  return (long long)(((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v));
+}
 
 // Group g's rows, clamped into [0, rows].
 __device__ __forceinline__ void mx4_group_rows(const Mx4Args& g, int e, long long& lo, long long& hi) {
@@ -131,6 +136,11 @@ __device__ __forceinline__ bool mx4_tile(const Mx4Args& g, long long b, int bm, 
     t.m0 = lo + (long long)mt * per;
     t.m_end = t.m0 + per < hi ? t.m0 + per : hi;
   }
+  // (in scalar registers: the tiles' buffer resources are made from them)
+  t.group = uniform(t.group);
+  t.nt = uniform(t.nt);
+  t.m0 = uniform(t.m0);
+  t.m_end = uniform(t.m_end);
   return true;
 }
 
@@ -233,8 +243,8 @@ __device__ __forceinline__ Mx4Lane mx4_lane(long long first, int row, bool count
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t mx4_rsrc(const uint8_t* p, long long first, int rows, int slices,
                                                            int unit) {
   const int blocks = rows > 0 ? ((int)(first & 31) + rows + 31) >> 5 : 1;
-  return __builtin_amdgcn_make_buffer_rsrc((void*)(p + (first >> 5) * slices * unit), (short)0, blocks * slices * unit,
-                                           kBufferRsrcWord3);
+  const long long at = uniform((long long)p + (first >> 5) * slices * unit);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)at, (short)0, uniform(blocks * slices * unit), kBufferRsrcWord3);
 }
 __device__ __forceinline__ u32x4 mx4_load(const __amdgpu_buffer_rsrc_t& rsrc, int lane_off, int off) {
   typedef uint32_t raw4 __attribute__((vector_size(16)));
@@ -262,7 +272,7 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int KT = g.slices;
   constexpr int BN = GATED ? 32 : 32 * NB;
-  const int n0 = __builtin_amdgcn_readfirstlane(t.nt) * BN;
+  const int n0 = t.nt * BN;
   const long long w_first = (long long)t.group * (GATED ? 2 : 1) * g.n + n0;
   const int m_rows = (int)(t.m_end - t.m0);
   const __amdgpu_buffer_rsrc_t a_rsrc = mx4_rsrc(g.a, t.m0, m_rows, KT, kMx4SliceBytes);
@@ -416,10 +426,10 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int KT = g.slices;
-  const int n0 = __builtin_amdgcn_readfirstlane(t.nt) * (GATED ? 128 : 256) + wave * (GATED ? 32 : 64);
-  const int group = __builtin_amdgcn_readfirstlane(t.group);
+  const int n0 = t.nt * (GATED ? 128 : 256) + wave * (GATED ? 32 : 64);
+  const int group = t.group;
   const long long m0 = t.m0;
-  const int m_rows = __builtin_amdgcn_readfirstlane((int)(t.m_end - t.m0));
+  const int m_rows = (int)(t.m_end - t.m0);
   const __amdgpu_buffer_rsrc_t a_rsrc = mx4_rsrc(g.a, m0, m_rows, KT, kMx4SliceBytes);
   const __amdgpu_buffer_rsrc_t as_rsrc = mx4_rsrc(g.as, m0, m_rows, KT, kMx4SliceScales);
   __amdgpu_buffer_rsrc_t w_rsrc[2], ws_rsrc[2];
@@ -442,9 +452,10 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
   f32x16_mx4 acc[MB][2];
 
   // Requests name slice kt; past the last one the lanes read nowhere, at the last one's place.
+  auto place = [&](int kt) { return uniform(kt < KT ? kt : KT - 1); };
   int w_at, full_codes, cut_codes, full_scales, cut_scales, wc[2], wsc[2];
   auto aim_w = [&](int kt) {
-    w_at = kt < KT ? kt : KT - 1;
+    w_at = place(kt);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       wc[j] = kt < KT ? wl[j].codes : kMx4Nowhere;
@@ -455,7 +466,7 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
   };
   int a_at;
   auto aim_a = [&](int kt) {
-    a_at = kt < KT ? kt : KT - 1;
+    a_at = place(kt);
     full_codes = kt < KT ? full.codes : kMx4Nowhere;
     cut_codes = kt < KT ? cut.codes : kMx4Nowhere;
   };
@@ -531,6 +542,7 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
     using C1 = std::integral_constant<int, 1>;
     using C2 = std::integral_constant<int, 2>;
     using C3 = std::integral_constant<int, 3>;
+    w_at = place(kt + 1);  // as aim_w left it: not carried from slice to slice, where it would take a vector register
     weave<2 * MB, MB, 4 + MB>(mul(C0{}), [&](auto b) { af[1][b] = here[(b * 4 + 1) * 64]; },
                               [&](auto i) {
                                 if constexpr (i < 2) load_w(i, 3, Q);
@@ -589,7 +601,7 @@ __global__ __launch_bounds__(256, MAXB <= 4 ? 2 : 1) void mx4_ring_kernel(Mx4Arg
   __shared__ u32x4 lds[kRingSlots * MAXB * 256];
   Mx4Tile t;
   if (!mx4_tile<false>(g, (long long)blockIdx.y * gridDim.x + blockIdx.x, 32 * MAXB, t)) return;
-  const int blocks = __builtin_amdgcn_readfirstlane((int)((t.m_end - t.m0 + 31) / 32));
+  const int blocks = (int)((t.m_end - t.m0 + 31) / 32);
   if (blocks <= 0) return;  // fewer rows than tiles: an even share of none
   weave_run<1, MAXB + 1>([&](auto mb) {
     constexpr int MB = decltype(mb)::value;
