@@ -27,20 +27,21 @@ struct Mx4Args {
   void* c;
   uint8_t* cs;
   const int32_t* offsets;  // null: one group of all rows
-  long long rows, ldc;
+  long long ldc;
+  int rows;
   int groups;
   int n;        // columns of the output; a group's weight rows are n, or 2 n with gate and up
   int slices;   // K / 256
   int n_tiles;  // column tiles, rounded up to a multiple of 8
-  bool vec;     // rows of c take whole vectors of four columns
+  bool vec;     // rows of c take whole 16-byte vectors
 };
 
 namespace {
 
 struct Mx4Tile {  // wave-uniform
   int group;
-  long long m0, m_end;  // rows
-  int nt;               // column tile
+  int m0, m_end;  // rows
+  int nt;         // column tile
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -48,15 +49,23 @@ __device__ __forceinline__ long long uniform(long long v) {
   return (long long)(((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v));
 }
 
-// Group g's rows, clamped into [0, rows].
-__device__ __forceinline__ void mx4_group_rows(const Mx4Args& g, int e, long long& lo, long long& hi) {
-  const long long a = g.offsets[e], b = g.offsets[e + 1];
-  lo = a < 0 ? 0 : a < g.rows ? a : g.rows;
-  hi = b < lo ? lo : b < g.rows ? b : g.rows;
+// Inclusive sum over the wave's lanes (register moves across lanes; see common.h).
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int dpp_plus(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xF, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+  v = dpp_plus<0x111, 0xF>(v);  // row_shr:1
+  v = dpp_plus<0x112, 0xF>(v);  // row_shr:2
+  v = dpp_plus<0x114, 0xF>(v);  // row_shr:4
+  v = dpp_plus<0x118, 0xF>(v);  // row_shr:8
+  v = dpp_plus<0x142, 0xA>(v);  // row_bcast:15
+  return dpp_plus<0x143, 0xC>(v);  // row_bcast:31
 }
 
-// The tile of workgroup b, if any, found by each wave from the offsets: 64 groups
-// at a time, a scan of their counts of row tiles of at most bm rows.
+// The tile of workgroup b, if any, found by each wave from the offsets: lane i
+// holds group i's rows, and a scan of the groups' counts of row tiles (of at most bm
+// rows) places the tile; with more than 64 groups, 64 at a time.
 //
 // STRIPED (streaming tiles): groups in order, within a group of mt row tiles column
 // tile 8 q + b % 8 for each q, with all its row tiles in a row: workgroup b runs on
@@ -65,82 +74,67 @@ __device__ __forceinline__ void mx4_group_rows(const Mx4Args& g, int e, long lon
 //
 // Otherwise (ring tiles): a group's rows are shared evenly among its row tiles; its
 // tiles run over blocks of four column tiles, in each row tile by row tile; and runs of
-// 32 consecutive tiles (8 row x 4 column tiles, the workgroups that one XCD's 32 CUs
-// hold at a time) are dealt to the XCDs in turn, so that an XCD's L2 serves each row
-// block to four workgroups and each weight panel to eight.  The last runs, when
-// they do not go round, are dealt tile by tile.
+// 32 consecutive tiles (8 row x 4 column tiles) are dealt to the XCDs in turn, so
+// that an XCD's L2 serves each row block to four workgroups and each weight panel to
+// eight.  The last runs, when they do not go round, are dealt tile by tile.
 template <bool STRIPED>
-__device__ __forceinline__ bool mx4_tile(const Mx4Args& g, long long b, int bm, Mx4Tile& t) {
+__device__ __forceinline__ bool mx4_tile(const Mx4Args& g, int b, int bm, Mx4Tile& t) {
   const int lane = lane_id();
-  long long lo = 0, hi = g.rows, local;
-  int e = 0, mt_e = 0;
-  // row tiles of all groups
-  long long m_total = 0;
-  if (!g.offsets) {
-    m_total = (g.rows + bm - 1) / bm;
-  } else if (!STRIPED) {
-    for (int g0 = 0; g0 < g.groups; g0 += kWave) {
-      long long l = 0, h = 0;
-      if (g0 + lane < g.groups) mx4_group_rows(g, g0 + lane, l, h);
-      m_total += __builtin_amdgcn_readlane(wave_inclusive_scan((int)((h - l + bm - 1) / bm)), 63);
+  int l = 0, h = 0, mt = 0, incl = 0;  // of group g0 + lane
+  auto count = [&](int g0) {
+    l = h = 0;
+    const int e = g0 + lane;
+    if (!g.offsets) {
+      h = lane == 0 ? g.rows : 0;
+    } else if (e < g.groups) {
+      const int a = g.offsets[e], z = g.offsets[e + 1];
+      l = min(max(a, 0), g.rows);
+      h = max(l, min(z, g.rows));
     }
-  }
-  long long L = b;
+    mt = (int)((unsigned)(h - l + bm - 1) / (unsigned)bm);
+    incl = wave_scan(mt);
+    return __builtin_amdgcn_readlane(incl, 63);
+  };
+  int m_here = count(0);
+  int L = b;
   if constexpr (!STRIPED) {
-    const long long total = m_total * g.n_tiles;
-    const int x = (int)(b & 7);
-    const long long slot = b >> 3, base = slot / kXcdGroup * (8 * kXcdGroup), j = slot % kXcdGroup;
+    int m_total = m_here;
+    if (g.groups > kWave) {
+      for (int g0 = kWave; g0 < g.groups; g0 += kWave) m_total += count(g0);
+      m_here = count(0);
+    }
+    const int total = m_total * g.n_tiles;
+    const int x = b & 7, slot = b >> 3, base = slot / kXcdGroup * (8 * kXcdGroup), j = slot % kXcdGroup;
     L = base + 8 * kXcdGroup <= total ? base + x * kXcdGroup + j : base + 8 * j + x;
     if (L >= total) return false;
   }
-  if (!g.offsets) {
-    if (L >= m_total * g.n_tiles) return false;
-    local = L;
-    mt_e = (int)m_total;
-  } else {
-    const long long want = L / g.n_tiles;  // row tiles before this one, over all groups
-    long long base = 0;
-    bool found = false;
-    for (int g0 = 0; g0 < g.groups; g0 += kWave) {
-      long long l = 0, h = 0;
-      if (g0 + lane < g.groups) mx4_group_rows(g, g0 + lane, l, h);
-      const int mt = (int)((h - l + bm - 1) / bm);
-      const int incl = wave_inclusive_scan(mt);
-      const uint64_t past = __ballot(base + incl > want);
-      if (past) {
-        const int src = __builtin_ctzll(past);
-        e = g0 + src;
-        mt_e = __builtin_amdgcn_readlane(mt, src);
-        local = L - (base + __builtin_amdgcn_readlane(incl, src) - mt_e) * g.n_tiles;
-        found = true;
-        break;
-      }
-      base += __builtin_amdgcn_readlane(incl, 63);
-    }
-    if (!found) return false;
-    mx4_group_rows(g, e, lo, hi);
+  int want = (int)((unsigned)L / (unsigned)g.n_tiles);  // row tiles before this one
+  int at = L - want * g.n_tiles, g0 = 0;
+  while (want >= m_here) {
+    want -= m_here;
+    g0 += kWave;
+    if (g0 >= g.groups) return false;
+    m_here = count(g0);
   }
-  t.group = e;
-  const int at = (int)local;
+  const int src = __builtin_ctzll(__ballot(incl > want));
+  const int mt_e = __builtin_amdgcn_readlane(mt, src);
+  const int lo = __builtin_amdgcn_readlane(l, src), hi = __builtin_amdgcn_readlane(h, src);
+  at += (want - (__builtin_amdgcn_readlane(incl, src) - mt_e)) * g.n_tiles;  // within the group
+  t.group = uniform(g0 + src);
   if constexpr (STRIPED) {
     const int j = at >> 3, q = j / mt_e;
-    t.nt = 8 * q + (at & 7);
-    t.m0 = lo + (long long)(j - q * mt_e) * bm;
-    t.m_end = t.m0 + bm < hi ? t.m0 + bm : hi;
+    t.nt = uniform(8 * q + (at & 7));
+    t.m0 = uniform(lo + (j - q * mt_e) * bm);
+    t.m_end = uniform(min(t.m0 + bm, hi));
   } else {
     const int q = at / (4 * mt_e), r = at - q * 4 * mt_e;
-    const int width = g.n_tiles - 4 * q < 4 ? g.n_tiles - 4 * q : 4;
-    const int mt = r / width;
-    t.nt = 4 * q + r - mt * width;
-    const int per = (int)((hi - lo + mt_e - 1) / mt_e);
-    t.m0 = lo + (long long)mt * per;
-    t.m_end = t.m0 + per < hi ? t.m0 + per : hi;
+    const int width = min(4, g.n_tiles - 4 * q);
+    const int mi = r / width;
+    t.nt = uniform(4 * q + r - mi * width);
+    const int per = (hi - lo + mt_e - 1) / mt_e;
+    t.m0 = uniform(lo + mi * per);
+    t.m_end = uniform(min(t.m0 + per, hi));
   }
-  // (in scalar registers: the tiles' buffer resources are made from them)
-  t.group = uniform(t.group);
-  t.nt = uniform(t.nt);
-  t.m0 = uniform(t.m0);
-  t.m_end = uniform(t.m_end);
   return true;
 }
 
@@ -166,6 +160,13 @@ __device__ __forceinline__ float mx4_silu_mul(float g, float u) {
   const float e = __builtin_amdgcn_exp2f(t);
   const float ex = t < 128.f ? __builtin_fmaf(e, lo * kLn2, e) : e;
   return g * __builtin_amdgcn_rcpf(1.f + ex) * u;
+}
+
+// Two values to bf16, nearest even, packed.
+__device__ __forceinline__ uint32_t mx4_bf16_pair(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
 // Store one 32 x 32 block: lane (r, h) holds v[4 q + t] = column col0 + 8 q + 4 h + t of `row`.
@@ -209,8 +210,7 @@ __device__ __forceinline__ void mx4_store(const Mx4Args& g, const float (&v)[16]
         } else {
           typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
           *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(g.c) + at + 8 * q) =
-              u32x2{(uint32_t)f32_to_bf16(v[4 * q]) | ((uint32_t)f32_to_bf16(v[4 * q + 1]) << 16),
-                    (uint32_t)f32_to_bf16(v[4 * q + 2]) | ((uint32_t)f32_to_bf16(v[4 * q + 3]) << 16)};
+              u32x2{mx4_bf16_pair(v[4 * q], v[4 * q + 1]), mx4_bf16_pair(v[4 * q + 2], v[4 * q + 3])};
         }
       } else {
 #pragma unroll
@@ -240,11 +240,21 @@ __device__ __forceinline__ Mx4Lane mx4_lane(long long first, int row, bool count
 // The resource of `rows` rows from `first` on, which starts at the block of the first.
 // At least one block (of which no lane reads anything where there is no row), so that
 // every slice's offset lies within it.
+struct Mx4Span {
+  void* base;
+  int bytes;
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(int bytes) const {
+    return __builtin_amdgcn_make_buffer_rsrc(base, (short)0, bytes, kBufferRsrcWord3);
+  }
+};
+__device__ __forceinline__ Mx4Span mx4_span(const uint8_t* p, long long first, int rows, int slices, int unit) {
+  const int blocks = rows > 0 ? ((int)(first & 31) + rows + 31) >> 5 : 1;
+  return Mx4Span{(void*)uniform((long long)p + (first >> 5) * slices * unit), uniform(blocks * slices * unit)};
+}
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t mx4_rsrc(const uint8_t* p, long long first, int rows, int slices,
                                                            int unit) {
-  const int blocks = rows > 0 ? ((int)(first & 31) + rows + 31) >> 5 : 1;
-  const long long at = uniform((long long)p + (first >> 5) * slices * unit);
-  return __builtin_amdgcn_make_buffer_rsrc((void*)at, (short)0, uniform(blocks * slices * unit), kBufferRsrcWord3);
+  const Mx4Span s = mx4_span(p, first, rows, slices, unit);
+  return s.rsrc(s.bytes);
 }
 __device__ __forceinline__ u32x4 mx4_load(const __amdgpu_buffer_rsrc_t& rsrc, int lane_off, int off) {
   typedef uint32_t raw4 __attribute__((vector_size(16)));
@@ -274,7 +284,7 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
   constexpr int BN = GATED ? 32 : 32 * NB;
   const int n0 = t.nt * BN;
   const long long w_first = (long long)t.group * (GATED ? 2 : 1) * g.n + n0;
-  const int m_rows = (int)(t.m_end - t.m0);
+  const int m_rows = t.m_end - t.m0;
   const __amdgpu_buffer_rsrc_t a_rsrc = mx4_rsrc(g.a, t.m0, m_rows, KT, kMx4SliceBytes);
   const __amdgpu_buffer_rsrc_t as_rsrc = mx4_rsrc(g.as, t.m0, m_rows, KT, kMx4SliceScales);
   Mx4Lane al[MB], wl[NB];
@@ -371,7 +381,7 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
   }
 #pragma unroll
   for (int m = 0; m < MB; ++m) {
-    const long long row = t.m0 + 32 * m + r;
+    const int row = t.m0 + 32 * m + r;
     const bool live = row < t.m_end;
     float v[16];
     if constexpr (GATED) {
@@ -394,11 +404,63 @@ template <int NB, bool GATED, int OUT>
 __global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args g) {
   extern __shared__ __align__(16) float lds[];
   Mx4Tile t;
-  if (!mx4_tile<true>(g, (long long)blockIdx.y * gridDim.x + blockIdx.x, kStreamRows, t)) return;
+  if (!mx4_tile<true>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), kStreamRows, t)) return;
   if (t.nt * (GATED ? 32 : 32 * NB) >= (OUT == kMx4Fp4 ? (g.n + kMx4Slice - 1) / kMx4Slice * kMx4Slice : g.n)) return;
   if (t.m_end - t.m0 <= 32) mx4_stream_tile<1, NB, GATED, OUT>(g, t, lds);
   else mx4_stream_tile<2, NB, GATED, OUT>(g, t, lds);
 }
+
+// 32 rows x COLS columns of results in LDS, on their way from the lanes that hold 4
+// columns of a row to lanes that store 16 bytes side by side: a wave's store then
+// covers whole 64-byte pieces of its rows, where straight from the registers it would
+// touch 32 rows with 16 (bf16) or 32 bytes each, and the L2's request rate bounded the
+// epilogue (it took 16,000 cycles of a 128 x 256 bf16 tile's 53,000).  Rows are 16 bytes
+// apart beyond their width, so that neither side conflicts on banks.
+template <int OUT, int COLS>
+struct Mx4Patch {
+  static constexpr int esz = OUT == kMx4F32 ? 4 : 2;
+  static constexpr int pitch = COLS * esz + 16;
+  static constexpr int bytes = OUT == kMx4Fp4 ? 0 : 32 * pitch;
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+  static __device__ __forceinline__ void put(uint8_t* part, const float (&v)[16], int col, int r, int h) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint8_t* p = part + r * pitch + (col + 8 * q + 4 * h) * esz;
+      if constexpr (OUT == kMx4F32)
+        *reinterpret_cast<f32x4_mx4*>(p) = f32x4_mx4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+      else
+        *reinterpret_cast<u32x2*>(p) = u32x2{mx4_bf16_pair(v[4 * q], v[4 * q + 1]), mx4_bf16_pair(v[4 * q + 2], v[4 * q + 3])};
+    }
+  }
+
+  // The first `rows` rows, from row `row` and column `col0` on, in the order in which
+  // the wave wrote them (its LDS operations complete in order).
+  static __device__ __forceinline__ void store(const Mx4Args& g, const uint8_t* part, int row, int rows, int col0,
+                                               int lane) {
+    __builtin_amdgcn_wave_barrier();
+    constexpr int per_row = COLS * esz / 16, at_once = 64 / per_row, each = 16 / esz;
+    const int col = col0 + lane % per_row * each;
+#pragma unroll
+    for (int i = 0; i < 32 / at_once; ++i) {
+      const int rr = i * at_once + lane / per_row;
+      const u32x4 q = *reinterpret_cast<const u32x4*>(part + rr * pitch + lane % per_row * 16);
+      if (rr >= rows) continue;
+      uint8_t* o = static_cast<uint8_t*>(g.c) + ((long long)(row + rr) * g.ldc + col) * esz;
+      if (g.vec && col + each <= g.n) {
+        store16(o, q);
+      } else {
+#pragma unroll
+        for (int e = 0; e < each; ++e)
+          if (col + e < g.n) {
+            if constexpr (OUT == kMx4F32) reinterpret_cast<uint32_t*>(o)[e] = q[e];
+            else reinterpret_cast<uint16_t*>(o)[e] = (uint16_t)(q[e / 2] >> (16 * (e & 1)));
+          }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+};
 
 // ------------------------------------------------------------------ ring tile
 
@@ -416,9 +478,9 @@ __global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args g) {
 // step 3, and the scales, during the next slice's step 0).  The slice's barrier
 // stands before step 3, when every wave holds the last operands of the slice: its
 // slot is free for slice kt + SA, and slice kt + 1, which each wave has waited for,
-// is complete.  Requests past the last slice carry a lane offset outside
-// the resource: they move no memory, and every slice has the same instructions, so the
-// counted waits are exact throughout.
+// is complete.  Requests past the last slice go to an empty resource: they move
+// no memory, and every slice has the same instructions, so the counted waits are exact
+// throughout.
 template <int MB, int SA, bool GATED, int OUT>
 __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t, u32x4* lds) {
   constexpr int kSlot = MB * 256;  // 16-byte units
@@ -428,13 +490,15 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
   const int KT = g.slices;
   const int n0 = t.nt * (GATED ? 128 : 256) + wave * (GATED ? 32 : 64);
   const int group = t.group;
-  const long long m0 = t.m0;
-  const int m_rows = (int)(t.m_end - t.m0);
-  const __amdgpu_buffer_rsrc_t a_rsrc = mx4_rsrc(g.a, m0, m_rows, KT, kMx4SliceBytes);
-  const __amdgpu_buffer_rsrc_t as_rsrc = mx4_rsrc(g.as, m0, m_rows, KT, kMx4SliceScales);
-  __amdgpu_buffer_rsrc_t w_rsrc[2], ws_rsrc[2];
+  const int m0 = t.m0;
+  const int m_rows = t.m_end - t.m0;
+  const Mx4Span a_span = mx4_span(g.a, m0, m_rows, KT, kMx4SliceBytes);
+  const Mx4Span as_span = mx4_span(g.as, m0, m_rows, KT, kMx4SliceScales);
+  Mx4Span w_span[2], ws_span[2];
   // Row block b is MB - 1 blocks at most past the first; only the last one may be cut short.
-  const Mx4Lane full = mx4_lane(m0, r, true, KT, h), cut = mx4_lane(m0, r, 32 * (MB - 1) + r < m_rows, KT, h);
+  Mx4Lane full = mx4_lane(m0, r, true, KT, h), cut = mx4_lane(m0, r, 32 * (MB - 1) + r < m_rows, KT, h);
+  full.codes += wave * 1024;  // of a slice of `a`, this wave moves step `wave`
+  cut.codes += wave * 1024;
   Mx4Lane wl[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -442,8 +506,8 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
     const int left = g.n - n0 - (GATED ? 0 : 32 * j);
     const int rows = left < 0 ? 0 : left < 32 ? left : 32;
     wl[j] = mx4_lane(first, r, r < rows, KT, h);
-    w_rsrc[j] = mx4_rsrc(g.w, first, rows, KT, kMx4SliceBytes);
-    ws_rsrc[j] = mx4_rsrc(g.ws, first, rows, KT, kMx4SliceScales);
+    w_span[j] = mx4_span(g.w, first, rows, KT, kMx4SliceBytes);
+    ws_span[j] = mx4_span(g.ws, first, rows, KT, kMx4SliceScales);
   }
 
   u32x4 wf[2][2][4];  // [slice parity][panel][step]
@@ -451,41 +515,36 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
   u32x4 af[2][MB];  // [step parity]
   f32x16_mx4 acc[MB][2];
 
-  // Requests name slice kt; past the last one the lanes read nowhere, at the last one's place.
-  auto place = [&](int kt) { return uniform(kt < KT ? kt : KT - 1); };
-  int w_at, full_codes, cut_codes, full_scales, cut_scales, wc[2], wsc[2];
-  auto aim_w = [&](int kt) {
-    w_at = place(kt);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      wc[j] = kt < KT ? wl[j].codes : kMx4Nowhere;
-      wsc[j] = kt < KT ? wl[j].scales : kMx4Nowhere;
-    }
-    full_scales = kt < KT ? full.scales : kMx4Nowhere;
-    cut_scales = kt < KT ? cut.scales : kMx4Nowhere;
-  };
-  int a_at;
+  // What the requests of `a` and the loads of weights and scales name now: a slice's place, and
+  // all of a resource; past the last slice its beginning, and nothing of it.  (All of it in
+  // scalar registers: the lane offsets, which the resource's length checks, stay the same.)
+  int a_slice, w_slice;
+  bool a_in, w_in;
   auto aim_a = [&](int kt) {
-    a_at = place(kt);
-    full_codes = kt < KT ? full.codes : kMx4Nowhere;
-    cut_codes = kt < KT ? cut.codes : kMx4Nowhere;
+    a_in = kt < KT;
+    a_slice = uniform(a_in ? kt : 0);
   };
-  // Row block b of `a`, of which this wave moves step `wave`.  The lane offset carries all that
-  // depends on the row: it is the part that is checked against the resource.
+  auto aim_w = [&](int kt) {
+    w_in = kt < KT;
+    w_slice = uniform(w_in ? kt : 0);
+  };
   auto request_a = [&](int b, int slot) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rsrc, MOEPD_LPTR(lds + slot * kSlot + (b * 4 + wave) * 64), 16,
-                                             (b == MB - 1 ? cut_codes : full_codes) + b * KT * kMx4SliceBytes,
-                                             a_at * kMx4SliceBytes + wave * 1024, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(a_span.rsrc(a_in ? a_span.bytes : 0),
+                                             MOEPD_LPTR(lds + slot * kSlot + (b * 4 + wave) * 64), 16,
+                                             (b == MB - 1 ? cut.codes : full.codes) + b * KT * kMx4SliceBytes,
+                                             a_slice * kMx4SliceBytes, 0, 0);
   };
   auto load_w = [&](int j, int s, int p) {
-    wf[p][j][s] = mx4_load(w_rsrc[j], wc[j], w_at * kMx4SliceBytes + s * 1024);
+    wf[p][j][s] = mx4_load(w_span[j].rsrc(w_in ? w_span[j].bytes : 0), wl[j].codes + s * 1024, w_slice * kMx4SliceBytes);
   };
   auto load_sw = [&](int j, int p) {
-    sw[p][j] = __builtin_amdgcn_raw_buffer_load_b32(ws_rsrc[j], wsc[j], w_at * kMx4SliceScales, 0);
+    sw[p][j] = __builtin_amdgcn_raw_buffer_load_b32(ws_span[j].rsrc(w_in ? ws_span[j].bytes : 0), wl[j].scales,
+                                                    w_slice * kMx4SliceScales, 0);
   };
   auto load_sa = [&](int b, int p) {
-    sa[p][b] = __builtin_amdgcn_raw_buffer_load_b32(
-        as_rsrc, (b == MB - 1 ? cut_scales : full_scales) + b * KT * kMx4SliceScales, w_at * kMx4SliceScales, 0);
+    sa[p][b] = __builtin_amdgcn_raw_buffer_load_b32(as_span.rsrc(w_in ? as_span.bytes : 0),
+                                                    (b == MB - 1 ? cut.scales : full.scales) + b * KT * kMx4SliceScales,
+                                                    w_slice * kMx4SliceScales, 0);
   };
 
   // In program order: the waits count requests.
@@ -542,7 +601,7 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
     using C1 = std::integral_constant<int, 1>;
     using C2 = std::integral_constant<int, 2>;
     using C3 = std::integral_constant<int, 3>;
-    w_at = place(kt + 1);  // as aim_w left it: not carried from slice to slice, where it would take a vector register
+    aim_w(kt + 1);  // as the last slice left it: not carried over, where it would take a vector register
     weave<2 * MB, MB, 4 + MB>(mul(C0{}), [&](auto b) { af[1][b] = here[(b * 4 + 1) * 64]; },
                               [&](auto i) {
                                 if constexpr (i < 2) load_w(i, 3, Q);
@@ -573,35 +632,44 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
   }
   if (kt < KT) slice(std::integral_constant<int, 0>{}, kt);
 
+  // The ring is free once every wave has left its last slice (whose requests past the
+  // end still write zeros to it): the waves pass their results through it, each in a part
+  // of its own, to store whole lines.
+  wait_vmcnt_lgkm0<0>();
+  bare_barrier();
+  constexpr int COLS = GATED ? 32 : 64;
+  uint8_t* part = reinterpret_cast<uint8_t*>(lds) + wave * Mx4Patch<OUT, COLS>::bytes;
 #pragma unroll
   for (int m = 0; m < MB; ++m) {
-    const bool live = 32 * m + r < m_rows;
-    const long long row = m0 + 32 * m + r;
     float v[16];
     if constexpr (GATED) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) v[i] = mx4_silu_mul(acc[m][0][i], acc[m][1][i]);
-      mx4_store<OUT>(g, v, row, live, n0, h);
+      if constexpr (OUT == kMx4Fp4) mx4_store<OUT>(g, v, m0 + 32 * m + r, 32 * m + r < m_rows, n0, h);
+      else Mx4Patch<OUT, COLS>::put(part, v, 0, r, h);
     } else {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = acc[m][j][i];
-        mx4_store<OUT>(g, v, row, live, n0 + 32 * j, h);
+        Mx4Patch<OUT, COLS>::put(part, v, 32 * j, r, h);
       }
     }
+    if constexpr (OUT != kMx4Fp4) Mx4Patch<OUT, COLS>::store(g, part, m0 + 32 * m, m_rows - 32 * m, n0, lane);
   }
 }
 
-// Tiles of up to 32 MAXB rows, cut to the 32-row blocks that they hold.  Up to 128
-// rows two workgroups share a CU; up to 256, one takes it.
+// Tiles of up to 32 MAXB rows, cut to the 32-row blocks that they hold.  Of the
+// 128-row kernel two workgroups share a CU, of the 64-row one three: one's start and
+// end, which take as long as eight slices, run beside another's slices.
 constexpr int kRingSlots = 3;
 template <int MAXB, bool GATED, int OUT>
-__global__ __launch_bounds__(256, MAXB <= 4 ? 2 : 1) void mx4_ring_kernel(Mx4Args g) {
-  __shared__ u32x4 lds[kRingSlots * MAXB * 256];
+__global__ __launch_bounds__(256, MAXB <= 2 ? 3 : 2) void mx4_ring_kernel(Mx4Args g) {
+  constexpr int ring = kRingSlots * MAXB * 256, parts = 4 * Mx4Patch<OUT, GATED ? 32 : 64>::bytes / 16;
+  __shared__ u32x4 lds[ring > parts ? ring : parts];
   Mx4Tile t;
-  if (!mx4_tile<false>(g, (long long)blockIdx.y * gridDim.x + blockIdx.x, 32 * MAXB, t)) return;
-  const int blocks = (int)((t.m_end - t.m0 + 31) / 32);
+  if (!mx4_tile<false>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), 32 * MAXB, t)) return;
+  const int blocks = (t.m_end - t.m0 + 31) / 32;
   if (blocks <= 0) return;  // fewer rows than tiles: an even share of none
   weave_run<1, MAXB + 1>([&](auto mb) {
     constexpr int MB = decltype(mb)::value;
@@ -617,12 +685,13 @@ hipError_t launch_mx4_gemm(Mx4Args g, bool gated, int out, hipStream_t s) {
   const long long width = out == kMx4Fp4 ? (g.n + kMx4Slice - 1) / kMx4Slice * kMx4Slice : g.n;
   // row tiles: at most one that is not full for each group that has a row
   const long long touched = g.groups < g.rows ? g.groups : g.rows;
-  const long long mean = g.rows / touched;
+  const int mean = (int)(g.rows / touched);
   auto launch = [&](auto kernel, int bm, int bn, int threads, size_t lds, int round) {
     g.n_tiles = (int)((width + bn - 1) / bn + round - 1) / round * round;
     const long long tiles = (g.rows / bm + touched) * g.n_tiles;
     // whole runs of 32 tiles to each XCD
     const long long blocks = round == 8 ? tiles : (tiles + 8 * kXcdGroup - 1) / (8 * kXcdGroup) * (8 * kXcdGroup);
+    if (blocks > 0x7fff0000LL) return hipErrorInvalidValue;
     kernel<<<grid_of(blocks, threads), threads, lds, s>>>(g);
     return hipGetLastError();
   };
@@ -637,8 +706,8 @@ hipError_t launch_mx4_gemm(Mx4Args g, bool gated, int out, hipStream_t s) {
   auto go = [&](auto gate, auto kind) {
     constexpr bool GATED = decltype(gate)::value;
     constexpr int OUT = decltype(kind)::value;
-    if (mean >= 160) return launch(mx4_ring_kernel<8, GATED, OUT>, 256, GATED ? 128 : 256, 256, 0, 1);
-    if (mean >= 32) return launch(mx4_ring_kernel<4, GATED, OUT>, 128, GATED ? 128 : 256, 256, 0, 1);
+    if (mean >= 64) return launch(mx4_ring_kernel<4, GATED, OUT>, 128, GATED ? 128 : 256, 256, 0, 1);
+    if (mean >= 32) return launch(mx4_ring_kernel<2, GATED, OUT>, 64, GATED ? 128 : 256, 256, 0, 1);
     if constexpr (GATED) return stream(mx4_stream_kernel<2, true, OUT>, 32, 2);
     else return few ? stream(mx4_stream_kernel<1, false, OUT>, 32, 1) : stream(mx4_stream_kernel<2, false, OUT>, 64, 2);
   };
@@ -684,14 +753,15 @@ int product(const uint8_t* a, const uint8_t* a_scales, int64_t rows, const uint8
   g.c = out;
   g.cs = out_scales;
   g.offsets = offsets;
-  g.rows = rows;
+  g.rows = (int)rows;
   g.ldc = out_stride;
   g.groups = groups;
   g.n = n;
   g.slices = mx4_slices(k);
-  g.vec = aligned(out, 4 * esz) && out_stride % 4 == 0;
+  g.vec = aligned(out, 16) && out_stride * esz % 16 == 0;
   const int kind = fp4 ? kMx4Fp4 : out_dtype == MOE_DTYPE_BF16 ? kMx4Bf16 : kMx4F32;
-  return launch_mx4_gemm(g, gated, kind, stream) == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+  const hipError_t st = launch_mx4_gemm(g, gated, kind, stream);
+  return st == hipSuccess ? MOE_OK : st == hipErrorInvalidValue ? MOE_ERR_INVALID_ARG : MOE_ERR_HIP;
 }
 
 }  // namespace
