@@ -95,6 +95,18 @@ __device__ __forceinline__ void load_logits(const BalanceArgs& g, int t, float (
   }
 }
 
+// exp(x) for x <= 0 (0 below -150): 2^(t + lo) with t + lo = x log2 e in two parts, so
+// that |x| does not multiply the product's rounding error; the hardware's 2^x adds 1 ulp.
+// NaN stays NaN.
+__device__ __forceinline__ float exp_of(float x) {
+  constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
+  x = x < -150.f ? -150.f : x;
+  const float t = x * kLog2e;
+  const float lo = __builtin_fmaf(x, kLog2eLow, __builtin_fmaf(x, kLog2e, -t));
+  const float e = __builtin_amdgcn_exp2f(t);
+  return __builtin_fmaf(e, lo * kLn2, e);
+}
+
 // Probabilities of a row in place; all zero where every logit is minus infinity,
 // NaN where one is NaN or plus infinity (the sum of the exponentials then is).
 template <int EPL>
@@ -107,7 +119,7 @@ __device__ __forceinline__ void softmax(float (&x)[EPL]) {
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
     // minus infinity against itself would be NaN: such a term is 0 (m, when NaN, is not equal to it)
-    x[i] = x[i] == -INFINITY ? 0.f : expf(x[i] - m);
+    x[i] = x[i] == -INFINITY ? 0.f : exp_of(x[i] - m);
     s += x[i];
   }
   s = wave_sum(s);
@@ -116,7 +128,10 @@ __device__ __forceinline__ void softmax(float (&x)[EPL]) {
   for (int i = 0; i < EPL; ++i) x[i] *= inv;
 }
 
-constexpr int kBalanceWaves = 4;
+constexpr int kBalanceWaves = 8;
+// Tokens that a wave has in flight at a time.
+template <int EPL>
+constexpr int kTokens = EPL <= 4 ? 4 : EPL == 8 ? 2 : 1;
 
 // A slot: E sums of probabilities, E counts, the live tokens.
 __host__ __device__ inline long long slot_words(int E) { return 2LL * E + 1; }
@@ -143,18 +158,28 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_pieces_kernel(Bala
 #pragma unroll
     for (int i = 0; i < EPL; ++i) acc[i] = 0.f;
     int live = 0;
-    for (int t = lo + wave; t < hi; t += kBalanceWaves) {
-      if (g.mask && !g.mask[t]) continue;
-      ++live;
-      float p[EPL];
-      load_logits<EPL, BF16>(g, t, p);
-      if (lane < g.k) {
-        const int e = idx[(long long)t * g.k + lane];
-        if ((uint32_t)e < (uint32_t)g.E) atomicAdd(&counts[e], 1);
-      }
-      softmax<EPL>(p);
+    constexpr int N = kTokens<EPL>;
+    for (int t0 = lo + wave * N; t0 < hi; t0 += kBalanceWaves * N) {
+      float p[N][EPL];
+      int e[N];
+      bool on[N];
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) acc[i] += p[i];
+      for (int j = 0; j < N; ++j) on[j] = t0 + j < hi && !(g.mask && !g.mask[t0 + j]);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if (!on[j]) continue;
+        load_logits<EPL, BF16>(g, t0 + j, p[j]);
+        e[j] = lane < g.k ? idx[(long long)(t0 + j) * g.k + lane] : -1;
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if (!on[j]) continue;
+        ++live;
+        if ((uint32_t)e[j] < (uint32_t)g.E) atomicAdd(&counts[e[j]], 1);
+        softmax<EPL>(p[j]);
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) acc[i] += p[j][i];
+      }
     }
 #pragma unroll
     for (int i = 0; i < EPL; ++i) sums[wave][lane + i * kWave] = acc[i];
@@ -197,14 +222,27 @@ __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceAr
   float p = 0.f;
   int cnt = 0, n = 0;
   if (lo < hi) {
+    // eight slots of a wave in flight; past the last one it reads that again
+    constexpr int N = 8;
     const int c1 = (hi - 1) / chunk;
-    for (int c = lo / chunk + wave; c <= c1; c += kJoinWaves) {
-      const uint32_t* slot = slots + (long long)(c + s) * slot_words(g.E);
-      if (e < g.E) {
-        p += __uint_as_float(slot[e]);
-        cnt += (int)slot[g.E + e];
+    const int at = e < g.E ? e : 0;
+    for (int c0 = lo / chunk + wave; c0 <= c1; c0 += kJoinWaves * N) {
+      float pv[N];
+      int cv[N], nv[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const uint32_t* slot = slots + (long long)(min(c0 + j * kJoinWaves, c1) + s) * slot_words(g.E);
+        pv[j] = __uint_as_float(slot[at]);
+        cv[j] = (int)slot[g.E + at];
+        nv[j] = (int)slot[2 * g.E];
       }
-      n += (int)slot[2 * g.E];
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const bool in = c0 + j * kJoinWaves <= c1;
+        p += in ? pv[j] : 0.f;
+        cnt += in ? cv[j] : 0;
+        n += in ? nv[j] : 0;
+      }
     }
   }
   ps[wave][lane] = p;
@@ -329,12 +367,12 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_backward_kernel(Ba
   }
 }
 
-// Tokens of a chunk: enough chunks to fill the GPU a few times over, at most
-// 1024, and at least four tokens to a wave.
+// Tokens of a chunk: at most 512 chunks (two workgroups to a CU; every slot is
+// written and read again), of whole rounds of its waves, one at least.
 int chunk_of(int T) {
-  const int most = 1024;
-  int c = (T + most - 1) / most;
-  return c < 4 * kBalanceWaves ? 4 * kBalanceWaves : c;
+  const int most = 512, round = 4 * kBalanceWaves;
+  const int c = (T + most - 1) / most;
+  return c <= round ? round : (c + round - 1) / round * round;
 }
 
 constexpr int kTicketBytes = 64;

@@ -72,6 +72,9 @@ __device__ __forceinline__ int wave_inclusive_scan(int v) {
 // stay in registers.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// The same at an element's alignment (global memory is read and written at any).
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
 __device__ __forceinline__ u32x4 load16(const void* p) { return *reinterpret_cast<const u32x4*>(p); }
 __device__ __forceinline__ void store16(void* p, const u32x4& v) { *reinterpret_cast<u32x4*>(p) = v; }
 

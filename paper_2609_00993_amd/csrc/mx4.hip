@@ -17,8 +17,7 @@ inline unsigned unit_grid(long long units) { return (unsigned)(units < (1 << 20)
 // Quantize.  A row's 256 values are read by half a wave, 8 consecutive values
 // to a lane, so four lanes share a block and find its maximum with two quad
 // permutations; the unit's codes cross LDS to leave as 4 KB of consecutive memory.
-// VEC: rows and strides are 16-byte aligned, so full groups of 8 are read as vectors.
-template <bool BF16, bool VEC>
+template <bool BF16>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restrict__ x, long long x_stride,
                                                            long long rows, int cols, int slices, long long units,
                                                            const int32_t* __restrict__ row_index,
@@ -48,17 +47,17 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restric
       for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
       if (src >= 0) {
         const long long at = src * x_stride + col;
-        if (VEC && col + 8 <= cols) {
+        if (col + 8 <= cols) {
           if constexpr (BF16) {
-            const u32x4 u = load16(static_cast<const uint16_t*>(x) + at);
+            const u32x4 u = *reinterpret_cast<const u32x4_any*>(static_cast<const uint16_t*>(x) + at);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               v[i][2 * j] = __uint_as_float(u[j] << 16);
               v[i][2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
             }
           } else {
-            const u32x4 a = load16(static_cast<const float*>(x) + at);
-            const u32x4 b = load16(static_cast<const float*>(x) + at + 4);
+            const u32x4 a = *reinterpret_cast<const u32x4_any*>(static_cast<const float*>(x) + at);
+            const u32x4 b = *reinterpret_cast<const u32x4_any*>(static_cast<const float*>(x) + at + 4);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               v[i][j] = __uint_as_float(a[j]);
@@ -125,7 +124,7 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* __restrict
 
 // The values: the unit's codes cross LDS so that half a wave writes a row's 256
 // values together.
-template <bool BF16, bool VEC>
+template <bool BF16>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __restrict__ codes,
                                                              const uint8_t* __restrict__ scales, long long rows,
                                                              int cols, int slices, long long units,
@@ -156,22 +155,22 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __re
         v[j] = ((w >> (4 * j)) & 8u ? -mag : mag) * s;
       }
       const long long at = row * out_stride + col;
-      if (VEC && col + 8 <= cols) {
+      if (col + 8 <= cols) {
         if constexpr (BF16) {
-          u32x4 q;
+          u32x4_any q;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             q[j] = (uint32_t)f32_to_bf16(v[2 * j]) | ((uint32_t)f32_to_bf16(v[2 * j + 1]) << 16);
-          store16(static_cast<uint16_t*>(out) + at, q);
+          __builtin_nontemporal_store(q, reinterpret_cast<u32x4_any*>(static_cast<uint16_t*>(out) + at));
         } else {
-          u32x4 a, b;
+          u32x4_any a, b;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             a[j] = __float_as_uint(v[j]);
             b[j] = __float_as_uint(v[4 + j]);
           }
-          store16(static_cast<float*>(out) + at, a);
-          store16(static_cast<float*>(out) + at + 4, b);
+          __builtin_nontemporal_store(a, reinterpret_cast<u32x4_any*>(static_cast<float*>(out) + at));
+          __builtin_nontemporal_store(b, reinterpret_cast<u32x4_any*>(static_cast<float*>(out) + at + 4));
         }
       } else {
 #pragma unroll
@@ -196,12 +195,10 @@ hipError_t launch_mx4_quantize(const void* x, bool bf16, long long x_stride, lon
   if (rows <= 0) return hipSuccess;
   const int slices = mx4_slices(cols);
   const long long units = (rows + kMx4Rows - 1) / kMx4Rows * slices;
-  const bool vec = aligned(x, 16) && x_stride * (bf16 ? 2 : 4) % 16 == 0;
   auto go = [&](auto k) {
     k<<<dim3(unit_grid(units)), 256, 0, s>>>(x, x_stride, rows, cols, slices, units, row_index, row_count, codes, scales);
   };
-  if (bf16) vec ? go(mx4_quantize_kernel<true, true>) : go(mx4_quantize_kernel<true, false>);
-  else vec ? go(mx4_quantize_kernel<false, true>) : go(mx4_quantize_kernel<false, false>);
+  bf16 ? go(mx4_quantize_kernel<true>) : go(mx4_quantize_kernel<false>);
   return hipGetLastError();
 }
 
@@ -272,12 +269,10 @@ int moe_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows
     return MOE_ERR_INVALID_ARG;
   const int slices = mx4_slices(cols);
   const long long units = (rows + kMx4Rows - 1) / kMx4Rows * slices;
-  const bool vec = aligned(out, 16) && out_stride * esz % 16 == 0;
   auto go = [&](auto k) {
     k<<<dim3(unit_grid(units)), 256, 0, stream>>>(codes, scales, rows, cols, slices, units, out, out_stride);
   };
-  if (esz == 2) vec ? go(mx4_dequantize_kernel<true, true>) : go(mx4_dequantize_kernel<true, false>);
-  else vec ? go(mx4_dequantize_kernel<false, true>) : go(mx4_dequantize_kernel<false, false>);
+  esz == 2 ? go(mx4_dequantize_kernel<true>) : go(mx4_dequantize_kernel<false>);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
