@@ -21,6 +21,7 @@
 #include "common.h"
 #include "kernels.h"
 #include "moepd_balance.h"
+#include "pipeline.h"
 
 namespace moepd {
 
@@ -41,13 +42,21 @@ __device__ __forceinline__ int seq_begin(const BalanceArgs& g, int s) {
   return v < 0 ? 0 : v < g.T ? v : g.T;
 }
 
-// The first sequence that ends past token t (S if none does).
+// The first sequence that ends past token t (S if none does).  The wave's lanes look
+// at 64 boundaries at a time, so that up to 64 sequences take one load and up to 4096
+// two, where a binary search would take one for each halving.
 __device__ __forceinline__ int seq_of(const BalanceArgs& g, int t) {
-  int lo = 0, hi = g.S;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (seq_begin(g, mid + 1) > t) hi = mid;
-    else lo = mid + 1;
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = g.S;  // the answer lies in [lo, lo + n]
+  while (n > 0) {
+    const int step = (n + kWave - 1) / kWave;
+    const int last = min((lane + 1) * step, n) - 1;  // of this lane's run of `step`
+    const uint64_t past = __ballot(lane * step < n && seq_begin(g, lo + last + 1) > t);
+    if (!past) return lo + n;
+    const int i = __builtin_ctzll(past);
+    lo += i * step;
+    if (step == 1) return lo;
+    n = min(step, n - i * step) - 1;  // its last one does: the answer at the latest
   }
   return lo;
 }
@@ -95,31 +104,22 @@ __device__ __forceinline__ void load_logits(const BalanceArgs& g, int t, float (
   }
 }
 
-// exp(x) for x <= 0 (0 below -150): 2^(t + lo) with t + lo = x log2 e in two parts, so
-// that |x| does not multiply the product's rounding error; the hardware's 2^x adds 1 ulp.
-// NaN stays NaN.
-__device__ __forceinline__ float exp_of(float x) {
-  constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
-  x = x < -150.f ? -150.f : x;
-  const float t = x * kLog2e;
-  const float lo = __builtin_fmaf(x, kLog2eLow, __builtin_fmaf(x, kLog2e, -t));
-  const float e = __builtin_amdgcn_exp2f(t);
-  return __builtin_fmaf(e, lo * kLn2, e);
-}
-
 // Probabilities of a row in place; all zero where every logit is minus infinity,
 // NaN where one is NaN or plus infinity (the sum of the exponentials then is).
+// e^(x - m) as 2^((x - m) log2 e): the two roundings and the constant's cost at most 2.2
+// |x - m| 2^-24 relative, so little where the probability is not small.
 template <int EPL>
 __device__ __forceinline__ void softmax(float (&x)[EPL]) {
+  constexpr float kLog2e = 1.44269504f;
   float m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) m = fmaxf(m, x[i]);
   m = wave_max(m);
+  m = m == -INFINITY ? 0.f : m;  // minus infinity against itself would be NaN
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
-    // minus infinity against itself would be NaN: such a term is 0 (m, when NaN, is not equal to it)
-    x[i] = x[i] == -INFINITY ? 0.f : exp_of(x[i] - m);
+    x[i] = __builtin_amdgcn_exp2f((x[i] - m) * kLog2e);
     s += x[i];
   }
   s = wave_sum(s);
@@ -133,72 +133,133 @@ constexpr int kBalanceWaves = 8;
 template <int EPL>
 constexpr int kTokens = EPL <= 4 ? 4 : EPL == 8 ? 2 : 1;
 
-// A slot: E sums of probabilities, E counts, the live tokens.
-__host__ __device__ inline long long slot_words(int E) { return 2LL * E + 1; }
+// A slot: E sums of probabilities, E counts, the live tokens, each part on lines of its own.
+__host__ __device__ inline int slot_counts(int E) { return (E + 31) / 32 * 32; }
+__host__ __device__ inline int slot_live(int E) { return 2 * slot_counts(E); }
+__host__ __device__ inline int slot_words(int E) { return slot_live(E) + 32; }
+
+// LDS of a workgroup that adds up a piece.
+template <int EPL, int WAVES>
+struct PieceSums {
+  float sums[WAVES][EPL * kWave];
+  int counts[EPL * kWave];
+  int live[WAVES];
+};
+
+// Tokens [lo, hi) of one sequence: every wave's sums and live tokens, and the counts, in LDS.
+template <int EPL, bool BF16, int WAVES>
+__device__ __forceinline__ void add_piece(const BalanceArgs& g, const int32_t* __restrict__ idx, int lo, int hi,
+                                          PieceSums<EPL, WAVES>& lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int e = threadIdx.x; e < g.E; e += 64 * WAVES) lds.counts[e] = 0;
+  __syncthreads();
+  float acc[EPL];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) acc[i] = 0.f;
+  int live = 0;
+  constexpr int N = kTokens<EPL>;
+  for (int t0 = lo + wave * N; t0 < hi; t0 += WAVES * N) {
+    float p[N][EPL];
+    int e[N];
+    bool on[N];
+    // the mask and what it may mask are read together
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int t = min(t0 + j, hi - 1);
+      on[j] = t0 + j < hi && !(g.mask && !g.mask[t]);
+      load_logits<EPL, BF16>(g, t, p[j]);
+      e[j] = lane < g.k ? idx[(long long)t * g.k + lane] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (!on[j]) continue;
+      ++live;
+      if ((uint32_t)e[j] < (uint32_t)g.E) atomicAdd(&lds.counts[e[j]], 1);
+      softmax<EPL>(p[j]);
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) acc[i] += p[j][i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) lds.sums[wave][lane + i * kWave] = acc[i];
+  if (lane == 0) lds.live[wave] = live;
+  __syncthreads();
+}
+template <int EPL, int WAVES>
+__device__ __forceinline__ float piece_sum(const PieceSums<EPL, WAVES>& lds, int e) {
+  float v = lds.sums[0][e];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) v += lds.sums[w][e];
+  return v;
+}
+template <int EPL, int WAVES>
+__device__ __forceinline__ int piece_live(const PieceSums<EPL, WAVES>& lds) {
+  int n = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) n += lds.live[w];
+  return n;
+}
+
+// f P = (E c / (k T_s)) (p / T_s) of an expert of a sequence with n live tokens
+// (counts and lengths are exact in float32 up to 2^24).
+__device__ __forceinline__ float load_of(const BalanceArgs& g, float p, int cnt, int n) {
+  return n ? (float)g.E * (float)cnt / ((float)g.k * (float)n) * (p * (1.f / (float)n)) : 0.f;
+}
 
 template <int EPL, bool BF16>
 __global__ __launch_bounds__(64 * kBalanceWaves) void balance_pieces_kernel(BalanceArgs g,
                                                                             const int32_t* __restrict__ idx, int chunk,
                                                                             uint32_t* __restrict__ slots,
                                                                             int32_t* __restrict__ ticket) {
-  __shared__ float sums[kBalanceWaves][EPL * kWave];
-  __shared__ int counts[EPL * kWave];
-  __shared__ int live_of[kBalanceWaves];
+  __shared__ PieceSums<EPL, kBalanceWaves> lds;
   if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = blockIdx.x;
   const int begin = c * chunk, end = min(begin + chunk, g.T);
   for (int s = seq_of(g, begin); s < g.S; ++s) {
     const int lo = max(begin, seq_begin(g, s)), hi = min(end, seq_begin(g, s + 1));
     if (lo >= end) break;
     if (lo >= hi) continue;  // an empty sequence
-    for (int e = threadIdx.x; e < g.E; e += 64 * kBalanceWaves) counts[e] = 0;
-    __syncthreads();
-    float acc[EPL];
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) acc[i] = 0.f;
-    int live = 0;
-    constexpr int N = kTokens<EPL>;
-    for (int t0 = lo + wave * N; t0 < hi; t0 += kBalanceWaves * N) {
-      float p[N][EPL];
-      int e[N];
-      bool on[N];
-#pragma unroll
-      for (int j = 0; j < N; ++j) on[j] = t0 + j < hi && !(g.mask && !g.mask[t0 + j]);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if (!on[j]) continue;
-        load_logits<EPL, BF16>(g, t0 + j, p[j]);
-        e[j] = lane < g.k ? idx[(long long)(t0 + j) * g.k + lane] : -1;
-      }
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if (!on[j]) continue;
-        ++live;
-        if ((uint32_t)e[j] < (uint32_t)g.E) atomicAdd(&counts[e[j]], 1);
-        softmax<EPL>(p[j]);
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) acc[i] += p[j][i];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) sums[wave][lane + i * kWave] = acc[i];
-    if (lane == 0) live_of[wave] = live;
-    __syncthreads();
+    add_piece<EPL, BF16>(g, idx, lo, hi, lds);
     uint32_t* slot = slots + (long long)(c + s) * slot_words(g.E);
     for (int e = threadIdx.x; e < g.E; e += 64 * kBalanceWaves) {
-      float v = sums[0][e];
-#pragma unroll
-      for (int w = 1; w < kBalanceWaves; ++w) v += sums[w][e];
-      slot[e] = __float_as_uint(v);
-      slot[g.E + e] = (uint32_t)counts[e];
+      slot[e] = __float_as_uint(piece_sum(lds, e));
+      slot[slot_counts(g.E) + e] = (uint32_t)lds.counts[e];
     }
-    if (threadIdx.x == 0) {
-      int n = 0;
-      for (int w = 0; w < kBalanceWaves; ++w) n += live_of[w];
-      slot[2 * g.E] = (uint32_t)n;
-    }
+    if (threadIdx.x == 0) slot[slot_live(g.E)] = (uint32_t)piece_live(lds);
     __syncthreads();  // the LDS is free for the next piece
+  }
+}
+
+// One sequence of few tokens: one workgroup does it all, with one launch.  64 tokens of 8
+// experts 9.4 us with two launches.
+constexpr int kSmallWaves = 16, kSmallTokens = 256;
+template <int EPL, bool BF16>
+__global__ __launch_bounds__(64 * kSmallWaves) void balance_small_kernel(BalanceArgs g, const int32_t* __restrict__ idx,
+                                                                       float* __restrict__ loss,
+                                                                       int32_t* __restrict__ counts,
+                                                                       int32_t* __restrict__ live) {
+  __shared__ PieceSums<EPL, kSmallWaves> lds;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lo = seq_begin(g, 0), hi = seq_begin(g, 1);
+  add_piece<EPL, BF16>(g, idx, lo, hi, lds);
+  const int n = piece_live(lds);
+  float v = 0.f;
+  for (int e = threadIdx.x; e < g.E; e += 64 * kSmallWaves) {
+    const int cnt = lds.counts[e];
+    counts[e] = cnt;
+    v += load_of(g, piece_sum(lds, e), cnt, n);
+  }
+  v = wave_sum(v);
+  __syncthreads();
+  if (lane == 0) lds.sums[0][wave] = v;  // the experts' sums have been read
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kSmallWaves; ++w) sum += lds.sums[0][w];
+    *loss = n ? g.coef * sum : 0.f;
+    live[0] = n;
+    live[1] = n > 0;
   }
 }
 
@@ -233,8 +294,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceAr
       for (int j = 0; j < N; ++j) {
         const uint32_t* slot = slots + (long long)(min(c0 + j * kJoinWaves, c1) + s) * slot_words(g.E);
         pv[j] = __uint_as_float(slot[at]);
-        cv[j] = (int)slot[g.E + at];
-        nv[j] = (int)slot[2 * g.E];
+        cv[j] = (int)slot[slot_counts(g.E) + at];
+        nv[j] = (int)slot[slot_live(g.E)];
       }
 #pragma unroll
       for (int j = 0; j < N; ++j) {
@@ -259,20 +320,21 @@ __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceAr
       n += ns[w];
     }
     if (e < g.E) counts[(long long)s * g.E + e] = cnt;
-    // f P = (E c / (k T_s)) (p / T_s); counts and lengths are exact in float32 up to 2^24
-    const float each = n ? 1.f / (float)n : 0.f;
-    const float f = (float)g.E * (float)cnt / ((float)g.k * (float)(n ? n : 1));
-    const float v = wave_sum(e < g.E && n ? f * (p * each) : 0.f);
+    const float v = wave_sum(e < g.E ? load_of(g, p, cnt, n) : 0.f);
     if (lane == 0) {
       __hip_atomic_store(&parts[(long long)s * groups + eg], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (eg == 0) __hip_atomic_store(&live[s], n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      // release this workgroup's results; the last to arrive acquires everyone's
-      last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == groups * g.S - 1;
+      // What the last workgroup reads is stored and loaded at the device's point of coherence, so
+      // all the ticket has to follow is those stores' completion: a release and an acquire for
+      // the whole device would write back and drop every XCD's L2 on the way.
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      wait_vmcnt_lgkm0<0>();
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == groups * g.S - 1;
     }
   }
   __syncthreads();
   if (!last) return;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   float sum = 0.f;
   int alive = 0;
   for (int i = threadIdx.x; i < groups * g.S; i += 64 * kJoinWaves)
@@ -312,6 +374,18 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_backward_kernel(Ba
   const long long first = ((long long)blockIdx.x * kBalanceWaves + wave) * run;
   if (first >= g.T) return;
   const int begin = (int)first, end = (int)(first + run < g.T ? first + run : g.T);
+  constexpr int N = EPL <= 8 ? 2 : 1;
+  float d[N][EPL];
+  uint8_t mask[N];
+  auto load = [&](int t0) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int t = min(t0 + j, end - 1);
+      mask[j] = g.mask ? g.mask[t] : 1;
+      load_logits<EPL, BF16>(g, t, d[j]);
+    }
+  };
+  load(begin);  // beside the loads that find its sequence
   const int seqs = live[g.S];
   const float scale = (grad ? *grad : 1.f) * g.coef;
   int s = seq_of(g, begin);
@@ -327,41 +401,46 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_backward_kernel(Ba
     }
   };
   enter();
-  for (int t = begin; t < end; ++t) {
-    if (t >= s_end && s < g.S) {
-      while (s < g.S && t >= s_end) {
-        ++s;
-        if (s < g.S) s_end = seq_begin(g, s + 1);
+  for (int t0 = begin; t0 < end; t0 += N) {
+    if (t0 != begin) load(t0);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int t = t0 + j;
+      if (t >= end) break;
+      if (t >= s_end && s < g.S) {
+        while (s < g.S && t >= s_end) {
+          ++s;
+          if (s < g.S) s_end = seq_begin(g, s + 1);
+        }
+        s_begin = s < g.S ? seq_begin(g, s) : g.T;
+        enter();
       }
-      s_begin = s < g.S ? seq_begin(g, s) : g.T;
-      enter();
-    }
-    const bool on = s < g.S && t >= s_begin && (!g.mask || g.mask[t]);
-    if (!on && accumulate) continue;
-    float d[EPL];
+      const bool on = s < g.S && t >= s_begin && mask[j];
+      if (!on && accumulate) continue;
+      if (on) {
+        softmax<EPL>(d[j]);
+        float dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) d[i] = 0.f;
-    if (on) {
-      load_logits<EPL, BF16>(g, t, d);
-      softmax<EPL>(d);
-      float dot = 0.f;
+        for (int i = 0; i < EPL; ++i) dot = __builtin_fmaf(f[i], d[j][i], dot);
+        dot = wave_sum(dot);
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) dot = __builtin_fmaf(f[i], d[i], dot);
-      dot = wave_sum(dot);
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) d[i] = weight * (d[i] * (f[i] - dot));
-    }
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      const int e = lane + i * kWave;
-      if (e >= g.E) continue;
-      const long long at = t * dstride + e;
-      if constexpr (BF16) {
-        uint16_t* o = static_cast<uint16_t*>(dlogits) + at;
-        *o = f32_to_bf16(accumulate ? bf16_to_f32(*o) + d[i] : d[i]);
+        for (int i = 0; i < EPL; ++i) d[j][i] = weight * (d[j][i] * (f[i] - dot));
       } else {
-        float* o = static_cast<float*>(dlogits) + at;
-        *o = accumulate ? *o + d[i] : d[i];
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) d[j][i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        const int e = lane + i * kWave;
+        if (e >= g.E) continue;
+        const long long at = t * dstride + e;
+        if constexpr (BF16) {
+          uint16_t* o = static_cast<uint16_t*>(dlogits) + at;
+          *o = f32_to_bf16(accumulate ? bf16_to_f32(*o) + d[j][i] : d[j][i]);
+        } else {
+          float* o = static_cast<float*>(dlogits) + at;
+          *o = accumulate ? *o + d[j][i] : d[j][i];
+        }
       }
     }
   }
@@ -375,7 +454,7 @@ int chunk_of(int T) {
   return c <= round ? round : (c + round - 1) / round * round;
 }
 
-constexpr int kTicketBytes = 64;
+constexpr int kTicketBytes = 128;
 
 int64_t workspace_bytes(int T, int E, int S) {
   const int chunk = chunk_of(T);
@@ -432,6 +511,16 @@ int moe_balance_loss(const void* logits, int32_t logits_dtype, int64_t logits_st
   int32_t* ticket = static_cast<int32_t*>(workspace);
   uint32_t* slots = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + kTicketBytes);
   float* parts = reinterpret_cast<float*>(slots + ((T + chunk - 1) / chunk + (long long)S) * slot_words(E));
+  if (S == 1 && T <= kSmallTokens) {
+    auto small = [&](auto epl) {
+      constexpr int EPL = decltype(epl)::value;
+      if (logits_dtype == MOE_DTYPE_BF16)
+        balance_small_kernel<EPL, true><<<1, 64 * kSmallWaves, 0, stream>>>(g, topk_idx, loss, counts, live);
+      else
+        balance_small_kernel<EPL, false><<<1, 64 * kSmallWaves, 0, stream>>>(g, topk_idx, loss, counts, live);
+    };
+    return by_experts(E, small) == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+  }
   auto pieces = [&](auto epl) {
     constexpr int EPL = decltype(epl)::value;
     if (logits_dtype == MOE_DTYPE_BF16)
