@@ -84,9 +84,11 @@ bool valid_config(const moe_config_t* c) {
   if (c->top_k < 1 || c->top_k > kMaxTopK || c->top_k > c->num_experts) return false;
   if (c->hidden < 64 || c->hidden > 16384 || c->hidden % 64) return false;
   if (c->inter < 64 || c->inter > 16384 || c->inter % 64) return false;
-  if (c->dtype != MOE_DTYPE_F32 && c->dtype != MOE_DTYPE_BF16 && c->dtype != MOE_DTYPE_FP8) return false;
+  if (c->dtype < MOE_DTYPE_F32 || c->dtype > MOE_DTYPE_FP4) return false;
   // MX FP8 GEMMs step through K 128 values at a time
   if (c->dtype == MOE_DTYPE_FP8 && (c->hidden % 128 || c->inter % 128)) return false;
+  // an MX FP4 matrix is held in whole slices of 256 columns
+  if (c->dtype == MOE_DTYPE_FP4 && (c->hidden % 256 || c->inter % 256)) return false;
   for (int p = 0; p < MOE_NUM_PHASES; ++p)
     if (c->max_tokens[p] < 0 || c->max_tokens[p] > (1 << 20)) return false;
   if (c->flags != 0) return false;
@@ -135,7 +137,11 @@ int alloc_phase(moe_ctx* ctx, int phase) {
   };
   const size_t o_idx = take(slots * 4), o_w = take(slots * 4), o_cnt = take(E * 4), o_off = take((E + 1) * 4);
   const size_t o_ros = take(slots * 4), o_tor = take(p.rows_cap * 4);
-  const size_t o_xp = take(p.rows_cap * c.hidden * ctx->esz), o_h = take(p.rows_cap * c.inter * ctx->esz);
+  const bool fp4 = c.dtype == MOE_DTYPE_FP4;
+  const size_t o_xp = take(fp4 ? mx4_code_bytes(p.rows_cap, c.hidden) + mx4_scale_bytes(p.rows_cap, c.hidden)
+                               : p.rows_cap * c.hidden * ctx->esz);
+  const size_t o_h = take(fp4 ? mx4_code_bytes(p.rows_cap, c.inter) + mx4_scale_bytes(p.rows_cap, c.inter)
+                              : p.rows_cap * c.inter * ctx->esz);
   const size_t o_y = take(p.rows_cap * c.hidden * 4);
   // Router GEMM: the logits, and room for its K-split partial products (at
   // least 4096 rows, so that small batches can split K many ways).
@@ -260,20 +266,27 @@ WindowSignal window_of(moe_ctx* ctx, int phase) {
 // sleeps 127 * 64 cycles, about 3.4 us at 2.4 GHz.  Not for tiles whose
 // workgroups hold too many registers for a D GEMM wave to share their SIMDs
 // (the bf16 256-row tiles, 464 and 392 VGPRs; the MX FP8 ring tiles, 408 to 512): a P
-// workgroup waiting on its CU would only keep D off it.
+// workgroup waiting on its CU would only keep D off it.  MX FP4 tiles do not wait: they
+// are short (the longest of 16,384 skewed tokens, hidden 7168, take about 40 us) and leave
+// a CU no room for D's.
 YieldTo yield_of(moe_ctx* ctx, int phase) {
   if (phase != MOE_PHASE_P || ctx->cfg.d_priority_us <= 0) return YieldTo{nullptr, 0, 0};
+  if (ctx->cfg.dtype == MOE_DTYPE_FP4) return YieldTo{nullptr, 0, 0};
   const int regime = ctx->ph[phase].regime;
   if (regime == 2 || (ctx->cfg.dtype == MOE_DTYPE_FP8 && regime == 0)) return YieldTo{nullptr, 0, 0};
   const Phase& d = ctx->ph[MOE_PHASE_D];
   return YieldTo{d.b.signal, d.gen, (ctx->cfg.d_priority_us * 10 + 33) / 34};
 }
 // MX FP8 contexts keep E4M3 codes and their scale bytes in the x_perm and h
-// regions (sized for bf16 rows, so codes plus scales fit).
+// regions (sized for bf16 rows, so codes plus scales fit), MX FP4 contexts the two
+// buffers of an MX FP4 matrix.
 MxBuffers mx_of(const moe_ctx* ctx, const Phase& p) {
   const size_t R = (size_t)p.rows_cap;
   uint8_t* xp = static_cast<uint8_t*>(p.b.x_perm);
   uint8_t* h = static_cast<uint8_t*>(p.b.h);
+  if (ctx->cfg.dtype == MOE_DTYPE_FP4)
+    return MxBuffers{xp, xp + mx4_code_bytes(p.rows_cap, ctx->cfg.hidden), h,
+                     h + mx4_code_bytes(p.rows_cap, ctx->cfg.inter)};
   return MxBuffers{xp, xp + R * ctx->cfg.hidden, h, h + R * ctx->cfg.inter};
 }
 
@@ -298,6 +311,10 @@ int layout(moe_ctx* ctx, Phase& p, hipStream_t stream) {
     p.regime = avg >= 512 ? 2 : avg >= 32 ? 0 : 1;
     p.bm = ffn_bf16_bm(p.regime, true);
     prefix32 = p.regime == 1;  // fewer than 32 x 1024 rows
+  } else if (c.dtype == MOE_DTYPE_FP4) {
+    // the products find their tiles from the offsets
+    p.regime = (long long)T * k / c.num_experts >= 32 ? 0 : 1;
+    p.bm = 32;
   } else {
     p.regime = 0;
     p.bm = ffn_f32_bm();
@@ -315,6 +332,32 @@ int layout(moe_ctx* ctx, Phase& p, hipStream_t stream) {
   });
 }
 
+// Rows that T tokens have at most on this GPU.
+long long most_rows(const moe_config_t& c, int T) {
+  return (long long)T * (c.top_k < c.num_local_experts ? c.top_k : c.num_local_experts);
+}
+
+// The expert products of an MX FP4 context.
+hipError_t ffn_mx4(const moe_ctx* ctx, const Phase& p, int gemm, hipStream_t stream) {
+  const moe_config_t& c = ctx->cfg;
+  const MxBuffers mx = mx_of(ctx, p);
+  Mx4Args g{};
+  g.offsets = p.b.offsets;
+  g.rows = (int)most_rows(c, p.T);
+  g.groups = c.num_local_experts;
+  g.a = gemm == 1 ? mx.x_codes : mx.h_codes;
+  g.as = gemm == 1 ? mx.x_scales : mx.h_scales;
+  g.w = static_cast<const uint8_t*>(gemm == 1 ? ctx->w.w_gate_up : ctx->w.w_down);
+  g.ws = static_cast<const uint8_t*>(gemm == 1 ? ctx->w.w_gate_up_scales : ctx->w.w_down_scales);
+  g.c = gemm == 1 ? static_cast<void*>(mx.h_codes) : p.b.y;
+  g.cs = gemm == 1 ? mx.h_scales : nullptr;
+  g.n = gemm == 1 ? c.inter : c.hidden;
+  g.ldc = g.n;
+  g.slices = (gemm == 1 ? c.hidden : c.inter) / 256;
+  const long long expect = (long long)p.T * c.top_k * c.num_local_experts / c.num_experts;  // under even routing
+  return launch_mx4_gemm(g, gemm == 1, gemm == 1 ? kMx4Fp4 : kMx4F32, expect, stream);
+}
+
 // Dispatch data movement: token rows into expert-contiguous rows.
 int permute(moe_ctx* ctx, Phase& p, const void* x, hipStream_t stream) {
   if (p.T == 0) return MOE_OK;
@@ -323,6 +366,14 @@ int permute(moe_ctx* ctx, Phase& p, const void* x, hipStream_t stream) {
     return timed(p, MOE_KERNEL_PERMUTE, stream, [&] {
       return launch_permute_mx(x, p.T, ctx->cfg.top_k, ctx->cfg.hidden, p.b.row_of_slot, mx.x_codes, mx.x_scales,
                                stream);
+    });
+  }
+  if (ctx->cfg.dtype == MOE_DTYPE_FP4) {
+    const MxBuffers mx = mx_of(ctx, p);
+    const moe_config_t& c = ctx->cfg;
+    return timed(p, MOE_KERNEL_PERMUTE, stream, [&] {
+      return launch_mx4_quantize(x, true, c.hidden, most_rows(c, p.T), c.hidden, p.b.token_of_row,
+                                 p.b.offsets + c.num_local_experts, mx.x_codes, mx.x_scales, stream);
     });
   }
   return timed(p, MOE_KERNEL_PERMUTE, stream, [&] {
@@ -338,12 +389,15 @@ int moe_ctx_create(const moe_config_t* cfg, const moe_weights_t* w, moe_ctx_t** 
   *out = nullptr;
   if (!cfg || !w || !w->w_gate_up || !w->w_down) return MOE_ERR_INVALID_ARG;
   if (!valid_config(cfg)) return MOE_ERR_INVALID_ARG;
-  if (cfg->dtype == MOE_DTYPE_FP8 && (!w->w_gate_up_scales || !w->w_down_scales)) return MOE_ERR_INVALID_ARG;
+  if (cfg->dtype >= MOE_DTYPE_FP8 && (!w->w_gate_up_scales || !w->w_down_scales)) return MOE_ERR_INVALID_ARG;
+  if (cfg->dtype == MOE_DTYPE_FP4 && ((uintptr_t)w->w_gate_up | (uintptr_t)w->w_down | (uintptr_t)w->w_gate_up_scales |
+                                      (uintptr_t)w->w_down_scales) % 16)
+    return MOE_ERR_INVALID_ARG;
   moe_ctx* ctx = new (std::nothrow) moe_ctx();
   if (!ctx) return MOE_ERR_OOM;
   ctx->cfg = *cfg;
   ctx->w = *w;
-  // bytes of an x element: FP8 contexts take bf16 hidden states
+  // bytes of an x element: FP8 and FP4 contexts take bf16 hidden states
   ctx->esz = cfg->dtype == MOE_DTYPE_F32 ? 4 : 2;
   if (hipGetDevice(&ctx->device) != hipSuccess) {
     delete ctx;
@@ -506,6 +560,7 @@ int moe_expert_ffn(moe_ctx_t* ctx, int phase, hipStream_t stream) {
                                MxWeights{ctx->w.w_gate_up, ctx->w.w_gate_up_scales, ctx->w.w_down, ctx->w.w_down_scales},
                                c.num_local_experts, c.hidden, c.inter, p.bm, max_m_tiles, m_tiles_hint, beside,
                                yield, stream);
+        if (c.dtype == MOE_DTYPE_FP4) return ffn_mx4(ctx, p, gemm, stream);
         if (c.dtype == MOE_DTYPE_BF16)
           return launch_ffn_bf16(p.regime, gemm, p.b, ctx->w.w_gate_up, ctx->w.w_down, c.num_local_experts, c.hidden,
                                  c.inter, max_m_tiles, m_tiles_hint, stage, share,
@@ -561,7 +616,7 @@ int moe_phase_view(const moe_ctx_t* ctx, int phase, moe_phase_view_t* v) {
   v->h = p.b.h;
   v->y = p.b.y;
   v->logits = p.b.logits;
-  if (ctx->cfg.dtype == MOE_DTYPE_FP8) {
+  if (ctx->cfg.dtype >= MOE_DTYPE_FP8) {
     const MxBuffers mx = mx_of(ctx, p);
     v->x_perm_scales = mx.x_scales;
     v->h_scales = mx.h_scales;

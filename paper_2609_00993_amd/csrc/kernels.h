@@ -196,6 +196,31 @@ hipError_t launch_mx4_quantize(const void* x, bool bf16, long long x_stride, lon
                                const int32_t* row_index, const int32_t* row_count, uint8_t* codes, uint8_t* scales,
                                hipStream_t s);
 
+// Products of MX FP4 matrices (see moe_mx4_gemm; gated: moe_mx4_gemm_swiglu).
+enum Mx4Out : int { kMx4F32 = 0, kMx4Bf16 = 1, kMx4Fp4 = 2 };
+struct Mx4Args {
+  const uint8_t* a;
+  const uint8_t* as;
+  const uint8_t* w;
+  const uint8_t* ws;
+  void* c;
+  uint8_t* cs;
+  const int32_t* offsets;  // null: one group of all rows
+  long long ldc;
+  int rows;
+  int groups;
+  int n;        // columns of the output; a group's weight rows are n, or 2 n with gate and up
+  int slices;   // K / 256
+  int n_tiles;  // column tiles (streaming tiles: rounded up to a multiple of 8); set by the launcher
+  int run;      // consecutive ring tiles that go to one XCD; set by the launcher
+};
+// expect: how many of the `rows` rows the offsets are expected to hold, which picks the
+// tiles (and nothing else: any offsets within the rows are computed).
+hipError_t launch_mx4_gemm(Mx4Args g, bool gated, int out, long long expect, hipStream_t s);
+// Code and scale bytes of an MX FP4 matrix.
+long long mx4_code_bytes(long long rows, int cols);
+long long mx4_scale_bytes(long long rows, int cols);
+
 int ffn_f32_bm();
 hipError_t launch_ffn_f32(int gemm, const PhaseBuffers& b, const void* w_gu, const void* w_dn, int e_loc, int H,
                           int I, int max_m_tiles, hipStream_t s);

@@ -202,6 +202,13 @@ hipError_t launch_mx4_quantize(const void* x, bool bf16, long long x_stride, lon
   return hipGetLastError();
 }
 
+long long mx4_code_bytes(long long rows, int cols) {
+  return (rows + kMx4Rows - 1) / kMx4Rows * mx4_slices(cols) * kMx4SliceBytes;
+}
+long long mx4_scale_bytes(long long rows, int cols) {
+  return (rows + kMx4Rows - 1) / kMx4Rows * mx4_slices(cols) * kMx4SliceScales;
+}
+
 }  // namespace moepd
 
 using namespace moepd;
@@ -220,9 +227,8 @@ extern "C" {
 
 int moe_mx4_size(int64_t rows, int32_t cols, int64_t* code_bytes, int64_t* scale_bytes) {
   if (!code_bytes || !scale_bytes || !valid_size(rows, cols)) return MOE_ERR_INVALID_ARG;
-  const int64_t units = (rows + kMx4Rows - 1) / kMx4Rows * mx4_slices(cols);
-  *code_bytes = units * kMx4SliceBytes;
-  *scale_bytes = units * kMx4SliceScales;
+  *code_bytes = mx4_code_bytes(rows, cols);
+  *scale_bytes = mx4_scale_bytes(rows, cols);
   return MOE_OK;
 }
 

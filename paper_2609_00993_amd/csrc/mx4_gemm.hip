@@ -17,25 +17,6 @@ typedef int32_t v8i32_mx4 __attribute__((ext_vector_type(8)));
 typedef float f32x16_mx4 __attribute__((ext_vector_type(16)));
 typedef float f32x4_mx4 __attribute__((ext_vector_type(4)));
 
-enum Mx4Out : int { kMx4F32 = 0, kMx4Bf16 = 1, kMx4Fp4 = 2 };
-
-struct Mx4Args {
-  const uint8_t* a;
-  const uint8_t* as;
-  const uint8_t* w;
-  const uint8_t* ws;
-  void* c;
-  uint8_t* cs;
-  const int32_t* offsets;  // null: one group of all rows
-  long long ldc;
-  int rows;
-  int groups;
-  int n;        // columns of the output; a group's weight rows are n, or 2 n with gate and up
-  int slices;   // K / 256
-  int n_tiles;  // column tiles (streaming tiles: rounded up to a multiple of 8)
-  int run;      // consecutive ring tiles that go to one XCD
-};
-
 namespace {
 
 struct Mx4Tile {  // wave-uniform
@@ -686,35 +667,37 @@ inline int up8(long long v) { return (int)((v + 7) / 8 * 8); }
 
 }  // namespace
 
-hipError_t launch_mx4_gemm(Mx4Args g, bool gated, int out, hipStream_t s) {
+hipError_t launch_mx4_gemm(Mx4Args g, bool gated, int out, long long expect, hipStream_t s) {
   const long long width = out == kMx4Fp4 ? (g.n + kMx4Slice - 1) / kMx4Slice * kMx4Slice : g.n;
-  // row tiles: at most one that is not full for each group that has a row
-  const long long touched = g.groups < g.rows ? g.groups : g.rows;
-  const int mean = (int)(g.rows / touched);
+  if (expect < 1) expect = 1;
+  if (expect > g.rows) expect = g.rows;
+  const long long touched = g.groups < expect ? g.groups : expect;  // groups that have a row
+  const int mean = (int)(expect / touched);
   auto launch = [&](auto kernel, int bm, int bn, int threads, size_t lds, int round) {
     g.n_tiles = (int)((width + bn - 1) / bn + round - 1) / round * round;
-    const long long tiles = (g.rows / bm + touched) * g.n_tiles;
     g.run = mean >= 512 ? 64 : 32;
+    // row tiles: at most one that is not full for each group that may have a row
+    const long long tiles = (g.rows / bm + (g.groups < g.rows ? g.groups : g.rows)) * g.n_tiles;
     const long long blocks = round == 8 ? tiles : (tiles + 8 * g.run - 1) / (8 * g.run) * (8 * g.run);  // whole rounds
     if (blocks > 0x7fff0000LL) return hipErrorInvalidValue;
     kernel<<<grid_of(blocks, threads), threads, lds, s>>>(g);
     return hipGetLastError();
   };
+  auto stream_tiles = [&](int bn) { return up8((width + bn - 1) / bn) * (expect / kStreamRows + touched); };
   auto stream = [&](auto kernel, int bn, int panels) {
-    const long long tiles = up8((width + bn - 1) / bn) * (g.rows / kStreamRows + touched);
     // enough waves to keep the memory busy: 8 to a CU
     int waves = 1;
-    while (waves < 8 && tiles * waves < 8 * 256 && waves * 2 <= g.slices) waves *= 2;
+    while (waves < 8 && stream_tiles(bn) * waves < 8 * 256 && waves * 2 <= g.slices) waves *= 2;
     return launch(kernel, kStreamRows, bn, 64 * waves, waves > 1 ? (size_t)waves * (kStreamRows / 32) * panels * 4096 : 0, 8);
   };
-  const bool few = up8((width + 63) / 64) * (g.rows / kStreamRows + touched) < 256;
   auto go = [&](auto gate, auto kind) {
     constexpr bool GATED = decltype(gate)::value;
     constexpr int OUT = decltype(kind)::value;
     if (mean >= 64) return launch(mx4_ring_kernel<4, GATED, OUT>, 128, GATED ? 128 : 256, 256, 0, 1);
     if (mean >= 32) return launch(mx4_ring_kernel<2, GATED, OUT>, 64, GATED ? 128 : 256, 256, 0, 1);
     if constexpr (GATED) return stream(mx4_stream_kernel<2, true, OUT>, 32, 2);
-    else return few ? stream(mx4_stream_kernel<1, false, OUT>, 32, 1) : stream(mx4_stream_kernel<2, false, OUT>, 64, 2);
+    else if (stream_tiles(64) < 256) return stream(mx4_stream_kernel<1, false, OUT>, 32, 1);
+    else return stream(mx4_stream_kernel<2, false, OUT>, 64, 2);
   };
   using Plain = std::false_type;
   using Gated = std::true_type;
@@ -764,7 +747,7 @@ int product(const uint8_t* a, const uint8_t* a_scales, int64_t rows, const uint8
   g.n = n;
   g.slices = mx4_slices(k);
   const int kind = fp4 ? kMx4Fp4 : out_dtype == MOE_DTYPE_BF16 ? kMx4Bf16 : kMx4F32;
-  const hipError_t st = launch_mx4_gemm(g, gated, kind, stream);
+  const hipError_t st = launch_mx4_gemm(g, gated, kind, rows, stream);
   return st == hipSuccess ? MOE_OK : st == hipErrorInvalidValue ? MOE_ERR_INVALID_ARG : MOE_ERR_HIP;
 }
 
