@@ -236,11 +236,6 @@ __device__ __forceinline__ Mx4Span mx4_span(const uint8_t* p, long long first, i
   const int blocks = rows > 0 ? ((int)(first & 31) + rows + 31) >> 5 : 1;
   return Mx4Span{(void*)uniform((long long)p + (first >> 5) * slices * unit), uniform(blocks * slices * unit)};
 }
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx4_rsrc(const uint8_t* p, long long first, int rows, int slices,
-                                                           int unit) {
-  const Mx4Span s = mx4_span(p, first, rows, slices, unit);
-  return s.rsrc(s.bytes);
-}
 __device__ __forceinline__ u32x4 mx4_load(const __amdgpu_buffer_rsrc_t& rsrc, int lane_off, int off) {
   typedef uint32_t raw4 __attribute__((vector_size(16)));
   const raw4 v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane_off, off, 0);
@@ -270,10 +265,10 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
   const int n0 = t.nt * BN;
   const long long w_first = (long long)t.group * (GATED ? 2 : 1) * g.n + n0;
   const int m_rows = t.m_end - t.m0;
-  const __amdgpu_buffer_rsrc_t a_rsrc = mx4_rsrc(g.a, t.m0, m_rows, KT, kMx4SliceBytes);
-  const __amdgpu_buffer_rsrc_t as_rsrc = mx4_rsrc(g.as, t.m0, m_rows, KT, kMx4SliceScales);
+  const Mx4Span a_span = mx4_span(g.a, t.m0, m_rows, KT, kMx4SliceBytes);
+  const Mx4Span as_span = mx4_span(g.as, t.m0, m_rows, KT, kMx4SliceScales);
   Mx4Lane al[MB], wl[NB];
-  __amdgpu_buffer_rsrc_t w_rsrc[NB], ws_rsrc[NB];
+  Mx4Span w_span[NB], ws_span[NB];
 #pragma unroll
   for (int m = 0; m < MB; ++m) al[m] = mx4_lane(t.m0, 32 * m + r, 32 * m + r < m_rows, KT, h);
 #pragma unroll
@@ -282,22 +277,29 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
     const int left = g.n - n0 - (GATED ? 0 : 32 * j);  // weight rows from the panel's first on
     const int rows = left < 0 ? 0 : left < 32 ? left : 32;
     wl[j] = mx4_lane(first, r, r < rows, KT, h);
-    w_rsrc[j] = mx4_rsrc(g.w, first, rows, KT, kMx4SliceBytes);
-    ws_rsrc[j] = mx4_rsrc(g.ws, first, rows, KT, kMx4SliceScales);
+    w_span[j] = mx4_span(g.w, first, rows, KT, kMx4SliceBytes);
+    ws_span[j] = mx4_span(g.ws, first, rows, KT, kMx4SliceScales);
   }
 
+  // A slice past the last one is the beginning of an empty resource: zeros, and no branch.
   auto load = [&](Mx4Slice4<MB, NB>& s, int kt) {
+    const bool in = kt < KT;
+    const int at = uniform(in ? kt : 0);
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      s.sw[j] = __builtin_amdgcn_raw_buffer_load_b32(ws_rsrc[j], wl[j].scales, kt * kMx4SliceScales, 0);
+      s.sw[j] = __builtin_amdgcn_raw_buffer_load_b32(ws_span[j].rsrc(in ? ws_span[j].bytes : 0), wl[j].scales,
+                                                     at * kMx4SliceScales, 0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s.w[j][i] = mx4_load(w_rsrc[j], wl[j].codes, kt * kMx4SliceBytes + i * 1024);
+      for (int i = 0; i < 4; ++i)
+        s.w[j][i] = mx4_load(w_span[j].rsrc(in ? w_span[j].bytes : 0), wl[j].codes + i * 1024, at * kMx4SliceBytes);
     }
 #pragma unroll
     for (int m = 0; m < MB; ++m) {
-      s.sa[m] = __builtin_amdgcn_raw_buffer_load_b32(as_rsrc, al[m].scales, kt * kMx4SliceScales, 0);
+      s.sa[m] = __builtin_amdgcn_raw_buffer_load_b32(as_span.rsrc(in ? as_span.bytes : 0), al[m].scales,
+                                                     at * kMx4SliceScales, 0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s.a[m][i] = mx4_load(a_rsrc, al[m].codes, kt * kMx4SliceBytes + i * 1024);
+      for (int i = 0; i < 4; ++i)
+        s.a[m][i] = mx4_load(a_span.rsrc(in ? a_span.bytes : 0), al[m].codes + i * 1024, at * kMx4SliceBytes);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -318,26 +320,24 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
     });
     __builtin_amdgcn_sched_barrier(0);
   };
-  Mx4Slice4<MB, NB> s0, s1;
-  // This wave's slices: wave, wave + waves, ...; the loop's loads carry no condition.
-  const int n = (KT - wave + waves - 1) / waves;
-  int kt = wave;
-  load(s0, kt);
-  if (n == 1) {
-    multiply(s0);
+  // This wave's slices: wave, wave + waves, ...
+  if (KT <= waves) {
+    Mx4Slice4<MB, NB> s;
+    load(s, wave);
+    multiply(s);
   } else {
+    Mx4Slice4<MB, NB> s0, s1;
+    int kt = wave;
+    load(s0, kt);
     load(s1, kt + waves);
-    int i = 0;
-    for (; i + 3 < n; i += 2, kt += 2 * waves) {
+    for (; kt + 2 * waves < KT; kt += 2 * waves) {
       multiply(s0);
       load(s0, kt + 2 * waves);
       multiply(s1);
       load(s1, kt + 3 * waves);
     }
     multiply(s0);
-    if (i + 2 < n) load(s0, kt + 2 * waves);
     multiply(s1);
-    if (i + 2 < n) multiply(s0);
   }
 
   if (waves > 1) {
@@ -384,15 +384,22 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
   }
 }
 
-constexpr int kStreamRows = 64;
-template <int NB, bool GATED, int OUT>
-__global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args g) {
+// Tiles of up to 32 MAXB rows: 32 where groups are expected to have few rows, since without
+// the 64-row body the kernel takes registers for three waves to a SIMD instead of two.
+constexpr int kStreamWaves = 8;
+template <int MAXB, int NB, bool GATED, int OUT>
+__global__ __launch_bounds__(64 * kStreamWaves, MAXB == 2 ? 2 : NB == 2 ? 3 : 4) void mx4_stream_kernel(
+    Mx4Args g) {
   extern __shared__ __align__(16) float lds[];
   Mx4Tile t;
-  if (!mx4_tile<true>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), kStreamRows, t)) return;
+  if (!mx4_tile<true>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), 32 * MAXB, t)) return;
   if (t.nt * (GATED ? 32 : 32 * NB) >= (OUT == kMx4Fp4 ? (g.n + kMx4Slice - 1) / kMx4Slice * kMx4Slice : g.n)) return;
-  if (t.m_end - t.m0 <= 32) mx4_stream_tile<1, NB, GATED, OUT>(g, t, lds);
-  else mx4_stream_tile<2, NB, GATED, OUT>(g, t, lds);
+  if constexpr (MAXB == 1) {
+    mx4_stream_tile<1, NB, GATED, OUT>(g, t, lds);
+  } else {
+    if (t.m_end - t.m0 <= 32) mx4_stream_tile<1, NB, GATED, OUT>(g, t, lds);
+    else mx4_stream_tile<2, NB, GATED, OUT>(g, t, lds);
+  }
 }
 
 // 32 rows x COLS columns of results in LDS, on their way from the lanes that hold 4
@@ -645,19 +652,20 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
   }
 }
 
-// Tiles of up to 32 MAXB rows, cut to the 32-row blocks that they hold.  Of the
-// 128-row kernel two workgroups share a CU, of the 64-row one three: one's start and
-// end, which take as long as eight slices, run beside another's slices.
-constexpr int kRingSlots = 3;
-template <int MAXB, bool GATED, int OUT>
-__global__ __launch_bounds__(256, MAXB <= 2 ? 3 : 2) void mx4_ring_kernel(Mx4Args g) {
-  constexpr int ring = kRingSlots * MAXB * 256, parts = 4 * Mx4Patch<OUT, GATED ? 32 : 64>::bytes / 16;
+// Tiles of up to 128 rows, cut to the 32-row blocks that they hold.  Two workgroups
+// share a CU: one's start and end, which take as long as eight slices, run beside the
+// other's slices (256-row tiles, one to a CU, took 150 us where these take 103: 8192 rows
+// over 32 groups, 7168 x 2048).
+constexpr int kRingSlots = 3, kRingBlocks = 4;
+template <bool GATED, int OUT>
+__global__ __launch_bounds__(256, 2) void mx4_ring_kernel(Mx4Args g) {
+  constexpr int ring = kRingSlots * kRingBlocks * 256, parts = 4 * Mx4Patch<OUT, GATED ? 32 : 64>::bytes / 16;
   __shared__ u32x4 lds[ring > parts ? ring : parts];
   Mx4Tile t;
-  if (!mx4_tile<false>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), 32 * MAXB, t)) return;
+  if (!mx4_tile<false>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), 32 * kRingBlocks, t)) return;
   const int blocks = (t.m_end - t.m0 + 31) / 32;
   if (blocks <= 0) return;  // fewer rows than tiles: an even share of none
-  weave_run<1, MAXB + 1>([&](auto mb) {
+  weave_run<1, kRingBlocks + 1>([&](auto mb) {
     constexpr int MB = decltype(mb)::value;
     if (blocks == MB) mx4_ring_tile<MB, kRingSlots, GATED, OUT>(g, t, lds);
   });
@@ -683,21 +691,33 @@ hipError_t launch_mx4_gemm(Mx4Args g, bool gated, int out, long long expect, hip
     kernel<<<grid_of(blocks, threads), threads, lds, s>>>(g);
     return hipGetLastError();
   };
-  auto stream_tiles = [&](int bn) { return up8((width + bn - 1) / bn) * (expect / kStreamRows + touched); };
-  auto stream = [&](auto kernel, int bn, int panels) {
-    // enough waves to keep the memory busy: 8 to a CU
+  // Expected tiles of bm rows and bn columns.
+  auto tiles_of = [&](int bm, int bn) { return (width + bn - 1) / bn * (expect / bm + touched); };
+  // Streaming tiles: waves to share a tile, enough to keep the memory busy, 8 to a CU.
+  auto stream = [&](auto kernel, int bm, int bn, int panels) {
     int waves = 1;
-    while (waves < 8 && stream_tiles(bn) * waves < 8 * 256 && waves * 2 <= g.slices) waves *= 2;
-    return launch(kernel, kStreamRows, bn, 64 * waves, waves > 1 ? (size_t)waves * (kStreamRows / 32) * panels * 4096 : 0, 8);
+    while (waves < kStreamWaves && tiles_of(bm, bn) * waves < 8 * 256 && waves * 2 <= g.slices) waves *= 2;
+    return launch(kernel, bm, bn, 64 * waves, waves > 1 ? (size_t)waves * (bm / 32) * panels * 4096 : 0, 8);
   };
+  // Ring tiles from 16 rows a group on (32 gated), if there are enough for many CUs.  us, ring / streaming tiles: 18
+  // rows in each of 64 groups, 2560 x 768, 18.4 / 19.3; 20 in each of 32, 7168 x 2048, 41.8 / 42.9, and
+  // gated, 2048 x 7168, 89.7 / 88.0; 28 in each of 64, gated, 768 x 2560, 31.4 / 29.0.  One matrix of
+  // 7168 x 7168: 128 rows (28 ring tiles) 28.6 / 18.2, 256 (56) 28.1 / 22.2, 512 (112) 28.6 / 36.1.
   auto go = [&](auto gate, auto kind) {
     constexpr bool GATED = decltype(gate)::value;
     constexpr int OUT = decltype(kind)::value;
-    if (mean >= 64) return launch(mx4_ring_kernel<4, GATED, OUT>, 128, GATED ? 128 : 256, 256, 0, 1);
-    if (mean >= 32) return launch(mx4_ring_kernel<2, GATED, OUT>, 64, GATED ? 128 : 256, 256, 0, 1);
-    if constexpr (GATED) return stream(mx4_stream_kernel<2, true, OUT>, 32, 2);
-    else if (stream_tiles(64) < 256) return stream(mx4_stream_kernel<1, false, OUT>, 32, 1);
-    else return stream(mx4_stream_kernel<2, false, OUT>, 64, 2);
+    if (mean >= (GATED ? 32 : 16) && tiles_of(128, GATED ? 128 : 256) >= 100)
+      return launch(mx4_ring_kernel<GATED, OUT>, 128, GATED ? 128 : 256, 256, 0, 1);
+    const bool tall = mean > 32;
+    if constexpr (GATED) {
+      return tall ? stream(mx4_stream_kernel<2, 2, true, OUT>, 64, 32, 2) : stream(mx4_stream_kernel<1, 2, true, OUT>, 32, 32, 2);
+    } else {
+      // panels of 32 columns where those of 64 would leave CUs idle
+      const bool narrow = tiles_of(tall ? 64 : 32, 64) < 256;
+      if (tall)
+        return narrow ? stream(mx4_stream_kernel<2, 1, false, OUT>, 64, 32, 1) : stream(mx4_stream_kernel<2, 2, false, OUT>, 64, 64, 2);
+      return narrow ? stream(mx4_stream_kernel<1, 1, false, OUT>, 32, 32, 1) : stream(mx4_stream_kernel<1, 2, false, OUT>, 32, 64, 2);
+    }
   };
   using Plain = std::false_type;
   using Gated = std::true_type;
