@@ -215,9 +215,10 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_pieces_kernel(Bala
   if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
   const int c = blockIdx.x;
   const int begin = c * chunk, end = min(begin + chunk, g.T);
-  for (int s = seq_of(g, begin); s < g.S; ++s) {
-    const int lo = max(begin, seq_begin(g, s)), hi = min(end, seq_begin(g, s + 1));
-    if (lo >= end) break;
+  int s = seq_of(g, begin);
+  for (int first = s < g.S ? seq_begin(g, s) : end; s < g.S && first < end; ++s) {
+    const int next = seq_begin(g, s + 1), lo = max(begin, first), hi = min(end, next);
+    first = next;
     if (lo >= hi) continue;  // an empty sequence
     add_piece<EPL, BF16>(g, idx, lo, hi, lds);
     uint32_t* slot = slots + (long long)(c + s) * slot_words(g.E);
@@ -230,9 +231,9 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_pieces_kernel(Bala
   }
 }
 
-// One sequence of few tokens: one workgroup does it all, with one launch.  64 tokens of 8
-// experts 9.4 us with two launches.
-constexpr int kSmallWaves = 16, kSmallTokens = 256;
+// One sequence of few tokens: one workgroup does it all, with one launch (64 tokens of 8
+// experts 4.4 us, two launches 8.4; 256 of 1024, 16 values to a lane, would take 24 and 9).
+constexpr int kSmallWaves = 16, kSmallRows = 256;
 template <int EPL, bool BF16>
 __global__ __launch_bounds__(64 * kSmallWaves) void balance_small_kernel(BalanceArgs g, const int32_t* __restrict__ idx,
                                                                        float* __restrict__ loss,
@@ -511,7 +512,7 @@ int moe_balance_loss(const void* logits, int32_t logits_dtype, int64_t logits_st
   int32_t* ticket = static_cast<int32_t*>(workspace);
   uint32_t* slots = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + kTicketBytes);
   float* parts = reinterpret_cast<float*>(slots + ((T + chunk - 1) / chunk + (long long)S) * slot_words(E));
-  if (S == 1 && T <= kSmallTokens) {
+  if (S == 1 && T * ((E + 63) / 64) <= kSmallRows) {
     auto small = [&](auto epl) {
       constexpr int EPL = decltype(epl)::value;
       if (logits_dtype == MOE_DTYPE_BF16)

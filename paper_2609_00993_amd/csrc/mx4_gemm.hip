@@ -100,7 +100,9 @@ __device__ __forceinline__ bool mx4_tile(const Mx4Args& g, int b, int bm, Mx4Til
     if (g0 >= g.groups) return false;
     m_here = count(g0);
   }
-  const int src = __builtin_ctzll(__ballot(incl > want));
+  const uint64_t past = __ballot(incl > want);
+  if (!past) return false;
+  const int src = __builtin_ctzll(past);
   const int mt_e = __builtin_amdgcn_readlane(mt, src);
   const int lo = __builtin_amdgcn_readlane(l, src), hi = __builtin_amdgcn_readlane(h, src);
   at += (want - (__builtin_amdgcn_readlane(incl, src) - mt_e)) * g.n_tiles;  // within the group

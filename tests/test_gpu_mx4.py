@@ -249,7 +249,8 @@ def _gated(y, bound, N):
 
 
 DENSE = [(1, 1, 32), (1, 33, 256), (2, 64, 257), (31, 100, 512), (32, 32, 768), (33, 65, 1024), (64, 257, 100),
-         (65, 31, 1280), (129, 128, 256), (300, 520, 1536), (513, 260, 768), (1, 700, 4096), (17, 1000, 2048)]
+         (65, 31, 1280), (129, 128, 256), (300, 520, 1536), (513, 260, 768), (1, 700, 4096), (17, 1000, 2048),
+         (300, 512, 4096), (40, 96, 4096)]
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])
@@ -337,6 +338,82 @@ def test_swiglu_into_fp4(env, kind, groups, rows, N, K):
     got = X.dequantize(c, s)
     assert (got >= X.e2m1_decode(X.e2m1_encode((ref - bound) / scale)) * scale).all()
     assert (got <= X.e2m1_decode(X.e2m1_encode((ref + bound) / scale)) * scale).all()
+
+
+@pytest.mark.parametrize("R,N", [(3, 40), (300, 520), (700, 4100)])
+def test_nan_rows_stay_nan_in_bf16(env, R, N):
+    """Of a matrix's rows one has a NaN block, in every tile form: its products are NaN, no other's."""
+    M, torch = env.M, env.torch
+    rng = np.random.default_rng(R)
+    K = 256
+    codes = rng.integers(0, 16, (R, K), dtype=np.uint8)
+    scales = np.full((R, K // 32), 127, np.uint8)
+    scales[R // 2, 3] = 255
+    a = [env.up(h) for h in X.hold(codes, scales)]
+    w, _ = _matrix(env, rng, 2 * N, K, 1)
+    for gated in (False, True):
+        y = torch.zeros((R, N), dtype=torch.bfloat16, device="cuda")
+        torch.cuda.synchronize()
+        if gated:
+            st = M.moe_mx4_gemm_swiglu(*a, R, *w, 1, None, N, K, y, None, M.MOE_DTYPE_BF16, 0, env.s)
+        else:
+            st = M.moe_mx4_gemm(*a, R, *w, 1, None, N, K, y, M.MOE_DTYPE_BF16, 0, env.s)
+        env.done(st, "product")
+        bad = torch.isnan(y).cpu().numpy()
+        assert bad[R // 2].all() and not np.delete(bad, R // 2, axis=0).any()
+
+
+def test_matrices_past_four_gigabytes(env):
+    """Codes, weights and results whose byte offsets pass 32 bits: the last rows are those of a small call."""
+    M, torch = env.M, env.torch
+    torch.manual_seed(5)
+    # 1,100,000 rows x 8192: 4.5 GB of codes, gathered from 64 rows
+    R, K, N = 1_100_000, 8192, 32
+    x = torch.randn((64, K), device="cuda", dtype=torch.bfloat16)
+    index = torch.randint(0, 64, (R,), dtype=torch.int32, device="cuda")
+    w, wv = _matrix(env, np.random.default_rng(1), N, K)
+    q, one = env.matrix(R, K, 0), env.matrix(64, K)
+    y, small = torch.empty((R, N), device="cuda"), torch.empty((64, N), device="cuda")
+    torch.cuda.synchronize()
+    assert q[0].numel() > 1 << 32
+    M.check(M.moe_mx4_quantize(x, M.MOE_DTYPE_BF16, 0, R, K, index, None, *q, env.s))
+    M.check(M.moe_mx4_gemm(*q, R, *w, 1, None, N, K, y, M.MOE_DTYPE_F32, 0, env.s))
+    M.check(M.moe_mx4_quantize(x, M.MOE_DTYPE_BF16, 0, 64, K, None, None, *one, env.s))
+    env.done(M.moe_mx4_gemm(*one, 64, *w, 1, None, N, K, small, M.MOE_DTYPE_F32, 0, env.s), "small")
+    # the same products, added in another order by other tiles
+    c, s = X.release(one[0].cpu().numpy(), one[1].cpu().numpy(), 64, K)
+    _, mag = X.product(X.dequantize(c, s), wv, [0, 64], N)
+    bound = torch.from_numpy(2 * _sum_bound(mag, K)).cuda()
+    pick = index.long()
+    for at in (slice(0, 1000), slice(R // 2, R // 2 + 1000), slice(R - 1000, R)):
+        assert ((y[at].double() - small[pick[at]].double()).abs() <= bound[pick[at]]).all()
+    del q, y
+    # 700 groups of 3200 weight rows x 4096: 4.6 GB; each group's row is the same, the last weights are known
+    G, N, K = 700, 3200, 4096
+    st, cb, sb = M.moe_mx4_size(G * N, K)
+    assert cb > 1 << 32
+    wc = torch.randint(0, 256, (cb,), dtype=torch.uint8, device="cuda")
+    ws = torch.randint(120, 130, (sb,), dtype=torch.uint8, device="cuda")
+    a, _ = _matrix(env, np.random.default_rng(2), G, K)
+    offs = torch.arange(G + 1, dtype=torch.int32, device="cuda")
+    y, small = torch.empty((G, N), device="cuda"), torch.empty((G, N), device="cuda")
+    torch.cuda.synchronize()
+    M.check(M.moe_mx4_gemm(*a, G, wc, ws, G, offs, N, K, y, M.MOE_DTYPE_F32, 0, env.s))
+    last = (cb // G * (G - 1), sb // G * (G - 1))
+    env.done(M.moe_mx4_gemm(*a, G, wc[last[0]:], ws[last[1]:], 1, None, N, K, small, M.MOE_DTYPE_F32, 0, env.s), "last")
+    scale = small[-1].abs().max()
+    assert float(scale) > 0 and float((y[-1] - small[-1]).abs().max()) <= 1e-4 * float(scale)
+    del wc, ws
+    # 700,001 rows x 3201 bf16 results: 4.5 GB
+    R, N, K = 700_001, 3201, 256
+    a, w = env.matrix(R, K, 0x35), _matrix(env, np.random.default_rng(3), N, K)[0]
+    a[1].fill_(127)
+    y = torch.zeros((R, N), dtype=torch.bfloat16, device="cuda")
+    small = torch.zeros((1, N), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    M.check(M.moe_mx4_gemm(*a, R, *w, 1, None, N, K, y, M.MOE_DTYPE_BF16, 0, env.s))
+    env.done(M.moe_mx4_gemm(*a, 1, *w, 1, None, N, K, small, M.MOE_DTYPE_BF16, 0, env.s), "row")
+    assert (y == small).all()  # every row is the same; one slice has one order
 
 
 def test_products_are_deterministic_and_graph_safe(env):
