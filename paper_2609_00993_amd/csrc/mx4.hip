@@ -27,22 +27,24 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restric
   __shared__ uint8_t bytes[kMx4SliceScales];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c8 = lane & 31;
-  long long used = rows;
-  if (row_count) {
-    const long long n = *row_count;
-    used = n < 0 ? 0 : n < rows ? n : rows;
-  }
   for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const long long rb = unit / slices;
     const int kt = (int)(unit - rb * slices);
+    // the row count and the indices are read together
+    int index[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const long long row = rb * kMx4Rows + 8 * wave + 2 * i + (lane >> 5);
+      index[i] = row_index && row < rows ? row_index[row] : -1;
+    }
+    const long long count = row_count ? *row_count : rows, used = count < rows ? count : rows;
     if (rb * kMx4Rows >= used) break;  // units ascend, so the whole workgroup is done
     const int col = kt * kMx4Slice + c8 * 8;
     float v[4][8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const long long row = rb * kMx4Rows + 8 * wave + 2 * i + (lane >> 5);
-      long long src = row < used ? row : -1;
-      if (row_index && src >= 0) src = row_index[row];
+      const long long src = row >= used ? -1 : row_index ? index[i] : row;
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
       if (src >= 0) {
