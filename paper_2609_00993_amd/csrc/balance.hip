@@ -3,7 +3,7 @@
 //
 // Both directions read the logits once; what bounds them is that stream, or, for
 // small batches, the launches.  One wave takes a token at a time, its logits in
-// registers (expert lane + 64 i in slot i), with wave-wide maxima and sums in
+// registers (runs of four neighbouring experts to a lane), with wave-wide maxima and sums in
 // cross-lane moves; lanes accumulate their own experts' probabilities, so the sum
 // over tokens crosses lanes only once per piece.
 //
@@ -89,17 +89,42 @@ __device__ __forceinline__ float wave_max(float v) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
+// A lane's EPL experts of a row: runs of V neighbours (16 bytes of float32), lane by lane.
+template <int EPL>
+constexpr int kRun = EPL < 4 ? EPL : 4;
+template <int EPL>
+__device__ __forceinline__ int expert_of(int i) {
+  constexpr int V = kRun<EPL>;
+  return i / V * (kWave * V) + (int)(threadIdx.x & 63) * V + i % V;
+}
+
 template <int EPL, bool BF16>
 __device__ __forceinline__ void load_logits(const BalanceArgs& g, int t, float (&x)[EPL]) {
-  const int lane = threadIdx.x & 63;
+  constexpr int V = kRun<EPL>;
 #pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    const int e = lane + i * kWave;
+  for (int i = 0; i < EPL; i += V) {
+    const int e = expert_of<EPL>(i);
     const long long at = t * g.stride + e;
-    x[i] = -INFINITY;
-    if (e < g.E) {
-      if constexpr (BF16) x[i] = bf16_to_f32(static_cast<const uint16_t*>(g.logits)[at]);
-      else x[i] = static_cast<const float*>(g.logits)[at];
+    if (V == 4 && e + V <= g.E) {
+      if constexpr (BF16) {
+        typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
+        const u16x4 q = *reinterpret_cast<const u16x4*>(static_cast<const uint16_t*>(g.logits) + at);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[i + j] = bf16_to_f32(q[j]);
+      } else {
+        const u32x4 q = *reinterpret_cast<const u32x4_any*>(static_cast<const float*>(g.logits) + at);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[i + j] = __uint_as_float(q[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        x[i + j] = -INFINITY;
+        if (e + j < g.E) {
+          if constexpr (BF16) x[i + j] = bf16_to_f32(static_cast<const uint16_t*>(g.logits)[at + j]);
+          else x[i + j] = static_cast<const float*>(g.logits)[at + j];
+        }
+      }
     }
   }
 }
@@ -131,7 +156,7 @@ __device__ __forceinline__ void softmax(float (&x)[EPL]) {
 constexpr int kBalanceWaves = 8;
 // Tokens that a wave has in flight at a time.
 template <int EPL>
-constexpr int kTokens = EPL <= 4 ? 4 : EPL == 8 ? 2 : 1;
+constexpr int kTokens = EPL <= 4 ? 4 : 2;
 
 // A slot: E sums of probabilities, E counts, the live tokens, each part on lines of its own.
 __host__ __device__ inline int slot_counts(int E) { return (E + 31) / 32 * 32; }
@@ -181,7 +206,7 @@ __device__ __forceinline__ void add_piece(const BalanceArgs& g, const int32_t* _
     }
   }
 #pragma unroll
-  for (int i = 0; i < EPL; ++i) lds.sums[wave][lane + i * kWave] = acc[i];
+  for (int i = 0; i < EPL; ++i) lds.sums[wave][expert_of<EPL>(i)] = acc[i];
   if (lane == 0) lds.live[wave] = live;
   __syncthreads();
 }
@@ -265,7 +290,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void balance_small_kernel(Balance
 }
 
 // Workgroup (x, s): 64 experts of sequence s.  Its waves deal the sequence's slots
-// among them, and their sums meet in LDS in wave order.
+// among them, and their sums meet in LDS in wave order.  16 waves, or 4 where there are
+// many sequences, whose workgroups fill the GPU by themselves.
 constexpr int kJoinWaves = 16;
 __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceArgs g, int chunk,
                                                                       const uint32_t* __restrict__ slots,
@@ -275,7 +301,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceAr
   __shared__ float ps[kJoinWaves][kWave];
   __shared__ int cs[kJoinWaves][kWave], ns[kJoinWaves];
   __shared__ int last;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int eg = blockIdx.x, groups = gridDim.x;
   const int s = blockIdx.y + gridDim.y * blockIdx.z;
   if (s >= g.S) return;
@@ -288,19 +314,19 @@ __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceAr
     constexpr int N = 8;
     const int c1 = (hi - 1) / chunk;
     const int at = e < g.E ? e : 0;
-    for (int c0 = lo / chunk + wave; c0 <= c1; c0 += kJoinWaves * N) {
+    for (int c0 = lo / chunk + wave; c0 <= c1; c0 += waves * N) {
       float pv[N];
       int cv[N], nv[N];
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const uint32_t* slot = slots + (long long)(min(c0 + j * kJoinWaves, c1) + s) * slot_words(g.E);
+        const uint32_t* slot = slots + (long long)(min(c0 + j * waves, c1) + s) * slot_words(g.E);
         pv[j] = __uint_as_float(slot[at]);
         cv[j] = (int)slot[slot_counts(g.E) + at];
         nv[j] = (int)slot[slot_live(g.E)];
       }
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const bool in = c0 + j * kJoinWaves <= c1;
+        const bool in = c0 + j * waves <= c1;
         p += in ? pv[j] : 0.f;
         cnt += in ? cv[j] : 0;
         n += in ? nv[j] : 0;
@@ -314,8 +340,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceAr
   if (wave == 0) {
     p = 0.f;
     cnt = n = 0;
-#pragma unroll
-    for (int w = 0; w < kJoinWaves; ++w) {
+    for (int w = 0; w < waves; ++w) {
       p += ps[w][lane];
       cnt += cs[w][lane];
       n += ns[w];
@@ -338,9 +363,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceAr
   if (!last) return;
   float sum = 0.f;
   int alive = 0;
-  for (int i = threadIdx.x; i < groups * g.S; i += 64 * kJoinWaves)
+  for (int i = threadIdx.x; i < groups * g.S; i += 64 * waves)
     sum += __hip_atomic_load(&parts[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  for (int i = threadIdx.x; i < g.S; i += 64 * kJoinWaves)
+  for (int i = threadIdx.x; i < g.S; i += 64 * waves)
     alive += __hip_atomic_load(&live[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 0;
   ps[wave][lane] = sum;
   cs[wave][lane] = alive;
@@ -348,8 +373,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceAr
   if (wave == 0) {
     sum = 0.f;
     alive = 0;
-#pragma unroll
-    for (int w = 0; w < kJoinWaves; ++w) {
+    for (int w = 0; w < waves; ++w) {
       sum += ps[w][lane];
       alive += cs[w][lane];
     }
@@ -371,11 +395,11 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_backward_kernel(Ba
                                                                               const float* __restrict__ grad,
                                                                               void* dlogits, long long dstride,
                                                                               bool accumulate) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wave = threadIdx.x >> 6;
   const long long first = ((long long)blockIdx.x * kBalanceWaves + wave) * run;
   if (first >= g.T) return;
   const int begin = (int)first, end = (int)(first + run < g.T ? first + run : g.T);
-  constexpr int N = EPL <= 8 ? 2 : 1;
+  constexpr int N = EPL <= 4 ? 4 : 2;
   float d[N][EPL];
   uint8_t mask[N];
   auto load = [&](int t0) {
@@ -397,7 +421,7 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_backward_kernel(Ba
     weight = n > 0 && seqs > 0 ? scale / ((float)n * (float)seqs) : 0.f;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
-      const int e = lane + i * kWave;
+      const int e = expert_of<EPL>(i);
       f[i] = e < g.E && n > 0 ? (float)g.E * (float)counts[(long long)s * g.E + e] / ((float)g.k * (float)n) : 0.f;
     }
   };
@@ -430,17 +454,29 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_backward_kernel(Ba
 #pragma unroll
         for (int i = 0; i < EPL; ++i) d[j][i] = 0.f;
       }
+      constexpr int V = kRun<EPL>;
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) {
-        const int e = lane + i * kWave;
-        if (e >= g.E) continue;
+      for (int i = 0; i < EPL; i += V) {
+        const int e = expert_of<EPL>(i);
         const long long at = t * dstride + e;
-        if constexpr (BF16) {
-          uint16_t* o = static_cast<uint16_t*>(dlogits) + at;
-          *o = f32_to_bf16(accumulate ? bf16_to_f32(*o) + d[j][i] : d[j][i]);
-        } else {
-          float* o = static_cast<float*>(dlogits) + at;
-          *o = accumulate ? *o + d[j][i] : d[j][i];
+        if (V == 4 && !BF16 && !accumulate && e + V <= g.E) {
+          // a gradient is written once, past the caches' keeping
+          const u32x4_any q = {__float_as_uint(d[j][i]), __float_as_uint(d[j][i + 1 % V]), __float_as_uint(d[j][i + 2 % V]),
+                               __float_as_uint(d[j][i + 3 % V])};
+          __builtin_nontemporal_store(q, reinterpret_cast<u32x4_any*>(static_cast<float*>(dlogits) + at));
+          continue;
+        }
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+          if (e + c >= g.E) continue;
+          const float v = d[j][i + c];
+          if constexpr (BF16) {
+            uint16_t* o = static_cast<uint16_t*>(dlogits) + at + c;
+            *o = f32_to_bf16(accumulate ? bf16_to_f32(*o) + v : v);
+          } else {
+            float* o = static_cast<float*>(dlogits) + at + c;
+            *o = accumulate ? *o + v : v;
+          }
         }
       }
     }
@@ -531,7 +567,8 @@ int moe_balance_loss(const void* logits, int32_t logits_dtype, int64_t logits_st
   };
   if (by_experts(E, pieces) != hipSuccess) return MOE_ERR_HIP;
   const int y = S < 1024 ? S : 1024;
-  balance_join_kernel<<<dim3(groups, y, (S + y - 1) / y), 64 * kJoinWaves, 0, stream>>>(g, chunk, slots, parts, ticket,
+  const int waves = (long long)groups * S > 512 ? 4 : kJoinWaves;
+  balance_join_kernel<<<dim3(groups, y, (S + y - 1) / y), 64 * waves, 0, stream>>>(g, chunk, slots, parts, ticket,
                                                                                       loss, counts, live);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
@@ -549,8 +586,8 @@ int moe_balance_loss_backward(const void* logits, int32_t logits_dtype, int64_t 
       ((uintptr_t)counts | (uintptr_t)live | (uintptr_t)grad) % 4)
     return MOE_ERR_INVALID_ARG;
   const BalanceArgs g{logits, token_mask, seq_offsets, logits_stride, S, T, E, k, coef};
-  // 8192 waves or one token each
-  const int run = (T + 8191) / 8192;
+  // 4096 waves or one token each
+  const int run = (T + 4095) / 4096;
   const int blocks = (int)(((T + run - 1) / run + kBalanceWaves - 1) / kBalanceWaves);
   auto go = [&](auto epl) {
     constexpr int EPL = decltype(epl)::value;
