@@ -11,8 +11,11 @@ namespace {
 
 constexpr int kUnitWords = 8 * 132;  // LDS words of a unit: a 32-value block of 32 rows, 128 words and 4 of padding
 
-// Units of a launch are walked with a grid stride.
-inline unsigned unit_grid(long long units) { return (unsigned)(units < (1 << 20) ? units : (1 << 20)); }
+// Units of a launch are walked with a grid stride, by two rounds of what the GPU holds
+// (2048 workgroups): a launch sized by a batch's capacity, of which a GPU's share may be an
+// eighth, then ends with its rows (65,536 rows of 7168, 8192 in use: 25 us, one
+// workgroup for each unit 55; all of 8243 in use 24 and 26).
+inline unsigned unit_grid(long long units) { return (unsigned)(units < 4096 ? units : 4096); }
 
 // Quantize.  A row's 256 values are read by half a wave, 8 consecutive values
 // to a lane, so four lanes share a block and find its maximum with two quad
