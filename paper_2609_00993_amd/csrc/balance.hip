@@ -2,7 +2,9 @@
 // (include/moepd_balance.h).
 //
 // Both directions read the logits once; what bounds them is that stream, or, for
-// small batches, the launches.  One wave takes a token at a time, its logits in
+// small batches, the launches and dependent loads.  65,536 x 256 float32: the pieces 15.5 us
+// (4.3 TB/s), their join 7.4, the gradient 24 (5.5 TB/s); 12,001 x 512 in 37 sequences 9.5,
+// 6 and 10.5; 64 x 8 in one launch 4.  One wave takes a token at a time, its logits in
 // registers (runs of four neighbouring experts to a lane), with wave-wide maxima and sums in
 // cross-lane moves; lanes accumulate their own experts' probabilities, so the sum
 // over tokens crosses lanes only once per piece.
@@ -11,7 +13,7 @@
 // chunk is cut where sequences end.  Chunk c and sequence s meet at most once,
 // and as tokens ascend either c or s does, so c + s numbers the pieces without a
 // gap in order: a piece's sums go to slot c + s, at most chunks + S - 1 slots.
-// The second kernel adds each sequence's slots in chunk order, so the
+// The second kernel adds each sequence's slots in a fixed order, so the
 // results do not depend on scheduling, and its last workgroup adds the sequences'
 // losses.  Sequences of any length mix: the work is dealt by tokens.
 #include <math.h>

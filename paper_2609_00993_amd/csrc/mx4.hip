@@ -1,6 +1,8 @@
 // MX FP4 matrices: quantizing rows, packing a checkpoint's codes, and the
-// values back (include/moepd_mx4.h).  All three move memory once; a workgroup
-// handles 32 rows x 256 values, the unit that is contiguous in the held order.
+// values back (include/moepd_mx4.h).  All three move memory once, which is what
+// bounds them, and for few rows the launch and three dependent loads (4 us for 64 rows
+// of 7168).  A workgroup handles 32 rows x 256 values, the unit that is contiguous in
+// the held order.
 #include "kernels.h"
 #include "moepd_mx4.h"
 #include "mx4.h"
@@ -20,6 +22,8 @@ inline unsigned unit_grid(long long units) { return (unsigned)(units < 4096 ? un
 // Quantize.  A row's 256 values are read by half a wave, 8 consecutive values
 // to a lane, so four lanes share a block and find its maximum with two quad
 // permutations; the unit's codes cross LDS to leave as 4 KB of consecutive memory.
+// 8243 rows of 7168 bf16 values gathered from 8192 24 us (6.2 TB/s of rows in and codes
+// out, some of the rows from the memory-side cache), 12,289 x 2559 float32 25 us (5.7).
 template <bool BF16>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restrict__ x, long long x_stride,
                                                            long long rows, int cols, int slices, long long units,
@@ -128,7 +132,7 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* __restrict
 }
 
 // The values: the unit's codes cross LDS so that half a wave writes a row's 256
-// values together.
+// values together (past the caches' keeping).  8243 x 7168 to bf16 37 us (4.1 TB/s).
 template <bool BF16>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __restrict__ codes,
                                                              const uint8_t* __restrict__ scales, long long rows,
