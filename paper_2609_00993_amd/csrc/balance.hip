@@ -291,93 +291,60 @@ __global__ __launch_bounds__(64 * kSmallWaves) void balance_small_kernel(Balance
   }
 }
 
-// Workgroup (x, s): 64 experts of sequence s.  Its waves deal the sequence's slots
-// among them, and their sums meet in LDS in wave order.  16 waves, or 4 where there are
-// many sequences, whose workgroups fill the GPU by themselves.
-constexpr int kJoinWaves = 16;
-__global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceArgs g, int chunk,
-                                                                      const uint32_t* __restrict__ slots,
-                                                                      float* __restrict__ parts, int32_t* ticket,
-                                                                      float* __restrict__ loss,
-                                                                      int32_t* __restrict__ counts, int32_t* live) {
-  __shared__ float ps[kJoinWaves][kWave];
-  __shared__ int cs[kJoinWaves][kWave], ns[kJoinWaves];
-  __shared__ int last;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int eg = blockIdx.x, groups = gridDim.x;
-  const int s = blockIdx.y + gridDim.y * blockIdx.z;
-  if (s >= g.S) return;
-  const int e = eg * kWave + lane;
+// A lane's expert e of sequence s: its sum, count and the live tokens over slots first,
+// first + step, ... of the sequence's, eight in flight (past the last one that again).
+__device__ __forceinline__ void add_slots(const BalanceArgs& g, int chunk, const uint32_t* __restrict__ slots, int s,
+                                          int e, int first, int step, float& p, int& cnt, int& n) {
   const int lo = seq_begin(g, s), hi = seq_begin(g, s + 1);
-  float p = 0.f;
-  int cnt = 0, n = 0;
-  if (lo < hi) {
-    // eight slots of a wave in flight; past the last one it reads that again
-    constexpr int N = 8;
-    const int c1 = (hi - 1) / chunk;
-    const int at = e < g.E ? e : 0;
-    for (int c0 = lo / chunk + wave; c0 <= c1; c0 += waves * N) {
-      float pv[N];
-      int cv[N], nv[N];
+  if (lo >= hi) return;
+  constexpr int N = 8;
+  const int c1 = (hi - 1) / chunk;
+  const int at = e < g.E ? e : 0;
+  for (int c0 = lo / chunk + first; c0 <= c1; c0 += step * N) {
+    float pv[N];
+    int cv[N], nv[N];
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const uint32_t* slot = slots + (long long)(min(c0 + j * waves, c1) + s) * slot_words(g.E);
-        pv[j] = __uint_as_float(slot[at]);
-        cv[j] = (int)slot[slot_counts(g.E) + at];
-        nv[j] = (int)slot[slot_live(g.E)];
-      }
+    for (int j = 0; j < N; ++j) {
+      const uint32_t* slot = slots + (long long)(min(c0 + j * step, c1) + s) * slot_words(g.E);
+      pv[j] = __uint_as_float(slot[at]);
+      cv[j] = (int)slot[slot_counts(g.E) + at];
+      nv[j] = (int)slot[slot_live(g.E)];
+    }
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const bool in = c0 + j * waves <= c1;
-        p += in ? pv[j] : 0.f;
-        cnt += in ? cv[j] : 0;
-        n += in ? nv[j] : 0;
-      }
+    for (int j = 0; j < N; ++j) {
+      const bool in = c0 + j * step <= c1;
+      p += in ? pv[j] : 0.f;
+      cnt += in ? cv[j] : 0;
+      n += in ? nv[j] : 0;
     }
   }
-  ps[wave][lane] = p;
-  cs[wave][lane] = cnt;
-  if (lane == 0) ns[wave] = n;
-  __syncthreads();
-  if (wave == 0) {
-    p = 0.f;
-    cnt = n = 0;
-    for (int w = 0; w < waves; ++w) {
-      p += ps[w][lane];
-      cnt += cs[w][lane];
-      n += ns[w];
-    }
-    if (e < g.E) counts[(long long)s * g.E + e] = cnt;
-    const float v = wave_sum(e < g.E ? load_of(g, p, cnt, n) : 0.f);
-    if (lane == 0) {
-      __hip_atomic_store(&parts[(long long)s * groups + eg], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (eg == 0) __hip_atomic_store(&live[s], n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      // What the last workgroup reads is stored and loaded at the device's point of coherence, so
-      // all the ticket has to follow is those stores' completion: a release and an acquire for
-      // the whole device would write back and drop every XCD's L2 on the way.
-      __atomic_signal_fence(__ATOMIC_SEQ_CST);
-      wait_vmcnt_lgkm0<0>();
-      __atomic_signal_fence(__ATOMIC_SEQ_CST);
-      last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == groups * g.S - 1;
-    }
-  }
-  __syncthreads();
-  if (!last) return;
+}
+
+constexpr int kJoinWaves = 16;
+struct JoinSums {
+  float p[kJoinWaves][kWave];
+  int counts[kJoinWaves][kWave], live[kJoinWaves];
+};
+
+// A workgroup adds all sequences' losses, in an order that its size alone decides.
+__device__ __forceinline__ void add_losses(const BalanceArgs& g, int groups, const float* parts, float* loss, int32_t* live,
+                                           JoinSums& lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   float sum = 0.f;
   int alive = 0;
   for (int i = threadIdx.x; i < groups * g.S; i += 64 * waves)
     sum += __hip_atomic_load(&parts[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   for (int i = threadIdx.x; i < g.S; i += 64 * waves)
     alive += __hip_atomic_load(&live[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 0;
-  ps[wave][lane] = sum;
-  cs[wave][lane] = alive;
+  lds.p[wave][lane] = sum;
+  lds.counts[wave][lane] = alive;
   __syncthreads();
   if (wave == 0) {
     sum = 0.f;
     alive = 0;
     for (int w = 0; w < waves; ++w) {
-      sum += ps[w][lane];
-      alive += cs[w][lane];
+      sum += lds.p[w][lane];
+      alive += lds.counts[w][lane];
     }
     sum = wave_sum(sum);
 #pragma unroll
@@ -387,6 +354,78 @@ __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceAr
       live[g.S] = alive;
     }
   }
+}
+
+// Workgroup (x, s): 64 experts of sequence s.  Its waves deal the sequence's slots
+// among them, their sums meet in LDS in wave order, and the last workgroup to finish adds
+// the losses.  16 waves, or 4 where the sequences' workgroups fill the GPU by themselves.
+__global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(BalanceArgs g, int chunk,
+                                                                      const uint32_t* __restrict__ slots,
+                                                                      float* __restrict__ parts, int32_t* ticket,
+                                                                      float* __restrict__ loss,
+                                                                      int32_t* __restrict__ counts, int32_t* live) {
+  __shared__ JoinSums lds;
+  __shared__ int last;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int eg = blockIdx.x, groups = gridDim.x, s = blockIdx.y;
+  const int e = eg * kWave + lane;
+  float p = 0.f;
+  int cnt = 0, n = 0;
+  add_slots(g, chunk, slots, s, e, wave, waves, p, cnt, n);
+  lds.p[wave][lane] = p;
+  lds.counts[wave][lane] = cnt;
+  if (lane == 0) lds.live[wave] = n;
+  __syncthreads();
+  if (wave == 0) {
+    p = 0.f;
+    cnt = n = 0;
+    for (int w = 0; w < waves; ++w) {
+      p += lds.p[w][lane];
+      cnt += lds.counts[w][lane];
+      n += lds.live[w];
+    }
+    if (e < g.E) counts[(long long)s * g.E + e] = cnt;
+    const float v = wave_sum(e < g.E ? load_of(g, p, cnt, n) : 0.f);
+    if (lane == 0) {
+      __hip_atomic_store(&parts[s * groups + eg], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (eg == 0) __hip_atomic_store(&live[s], n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      // What the last workgroup reads is stored and loaded at the device's point of coherence, so
+      // all the ticket has to follow is those stores' completion: a release and an acquire for
+      // the whole device would write back and drop every XCD's L2 on the way (12 us for 7).
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      wait_vmcnt_lgkm0<0>();
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == groups * g.S - 1;
+    }
+  }
+  __syncthreads();
+  if (last) add_losses(g, groups, parts, loss, live, lds);
+}
+
+// Many sequences: a wave each for 64 experts of a sequence, and a launch of its own for
+// the losses, since thousands of tickets on one word would take longer.
+__global__ __launch_bounds__(256) void balance_join_each_kernel(BalanceArgs g, int chunk,
+                                                               const uint32_t* __restrict__ slots,
+                                                               float* __restrict__ parts, int32_t* __restrict__ counts,
+                                                               int32_t* __restrict__ live) {
+  const int lane = threadIdx.x & 63;
+  const int eg = blockIdx.x, groups = gridDim.x, s = blockIdx.y * 4 + (threadIdx.x >> 6);
+  if (s >= g.S) return;  // whole wave leaves together
+  const int e = eg * kWave + lane;
+  float p = 0.f;
+  int cnt = 0, n = 0;
+  add_slots(g, chunk, slots, s, e, 0, 1, p, cnt, n);
+  if (e < g.E) counts[(long long)s * g.E + e] = cnt;
+  const float v = wave_sum(e < g.E ? load_of(g, p, cnt, n) : 0.f);
+  if (lane == 0) {
+    parts[s * groups + eg] = v;
+    if (eg == 0) live[s] = n;
+  }
+}
+__global__ __launch_bounds__(64 * kJoinWaves) void balance_total_kernel(BalanceArgs g, int groups, const float* parts,
+                                                                       float* loss, int32_t* live) {
+  __shared__ JoinSums lds;
+  add_losses(g, groups, parts, loss, live, lds);
 }
 
 // One wave takes a run of consecutive tokens, so that a sequence's f stays in its registers.
@@ -486,17 +525,23 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_backward_kernel(Ba
 }
 
 // Tokens of a chunk: at most 512 chunks (two workgroups to a CU; every slot is
-// written and read again), of whole rounds of its waves, one at least.
-int chunk_of(int T) {
-  const int most = 512, round = 4 * kBalanceWaves;
+// written and read again), of whole rounds of its waves, one at least.  A chunk's
+// sequences are taken one after another, 2 to 3 us each, so where sequences are shorter than
+// a round a chunk holds about two of them, and many sequences may have up to 4096 chunks (342
+// tokens in 126 sequences: 41 us with chunks of 32 tokens, 19 with 5; 60,000 tokens in 9000 sequences 179 and 52, with the
+// join of its own for many sequences).
+int chunk_of(int T, int S) {
+  const int most = S < 512 ? 512 : S < 4096 ? S : 4096, round = 4 * kBalanceWaves;
   const int c = (T + most - 1) / most;
-  return c <= round ? round : (c + round - 1) / round * round;
+  const long long two = S > 1 ? 2LL * T / S : round;
+  const int least = two < 4 ? 4 : two < round ? (int)two : round;
+  return c <= least ? least : c < round ? c : (c + round - 1) / round * round;
 }
 
 constexpr int kTicketBytes = 128;
 
 int64_t workspace_bytes(int T, int E, int S) {
-  const int chunk = chunk_of(T);
+  const int chunk = chunk_of(T, S);
   const int64_t slots = (T + chunk - 1) / chunk + (int64_t)S;
   return kTicketBytes + slots * slot_words(E) * 4 + (int64_t)S * ((E + 63) / 64) * 4;
 }
@@ -546,7 +591,7 @@ int moe_balance_loss(const void* logits, int32_t logits_dtype, int64_t logits_st
   if (T > 0 && (!logits || !topk_idx || !aligned(logits, logits_dtype))) return MOE_ERR_INVALID_ARG;
   if (ws_bytes < workspace_bytes(T, E, S)) return MOE_ERR_CAPACITY;
   const BalanceArgs g{logits, token_mask, seq_offsets, logits_stride, S, T, E, k, coef};
-  const int chunk = chunk_of(T), chunks = T > 0 ? (T + chunk - 1) / chunk : 1, groups = (E + 63) / 64;
+  const int chunk = chunk_of(T, S), chunks = T > 0 ? (T + chunk - 1) / chunk : 1, groups = (E + 63) / 64;
   int32_t* ticket = static_cast<int32_t*>(workspace);
   uint32_t* slots = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + kTicketBytes);
   float* parts = reinterpret_cast<float*>(slots + ((T + chunk - 1) / chunk + (long long)S) * slot_words(E));
@@ -568,10 +613,13 @@ int moe_balance_loss(const void* logits, int32_t logits_dtype, int64_t logits_st
       balance_pieces_kernel<EPL, false><<<chunks, 64 * kBalanceWaves, 0, stream>>>(g, topk_idx, chunk, slots, ticket);
   };
   if (by_experts(E, pieces) != hipSuccess) return MOE_ERR_HIP;
-  const int y = S < 1024 ? S : 1024;
-  const int waves = (long long)groups * S > 512 ? 4 : kJoinWaves;
-  balance_join_kernel<<<dim3(groups, y, (S + y - 1) / y), 64 * waves, 0, stream>>>(g, chunk, slots, parts, ticket,
-                                                                                      loss, counts, live);
+  if ((long long)groups * S > 4096) {
+    balance_join_each_kernel<<<dim3(groups, (S + 3) / 4), 256, 0, stream>>>(g, chunk, slots, parts, counts, live);
+    balance_total_kernel<<<1, 64 * kJoinWaves, 0, stream>>>(g, groups, parts, loss, live);
+  } else {
+    const int waves = groups * S > 512 ? 4 : kJoinWaves;
+    balance_join_kernel<<<dim3(groups, S), 64 * waves, 0, stream>>>(g, chunk, slots, parts, ticket, loss, counts, live);
+  }
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

@@ -127,7 +127,7 @@ def test_loss_and_gradient(T, E, k, dtype):
 
 
 @pytest.mark.parametrize("T,E,S", [(40, 7, 3), (200, 65, 11), (333, 130, 40), (64, 16, 64), (90, 300, 200), (2100, 12, 5),
-                                   (700, 20, 1300)])
+                                   (700, 20, 1300), (5000, 70, 2500), (40, 5, 6000)])
 def test_sequences_and_masks(T, E, S):
     """Sequences of any length, empty ones and fully masked ones among them, tokens of none at both ends."""
     rng = np.random.default_rng(T + S)
