@@ -19,8 +19,8 @@
  * logits are all minus infinity has probability 0 everywhere.  Other infinities
  * and NaN in a live token's logits give NaN.
  *
- * Conventions: as in moepd.h; no state, no allocation, no synchronisation, and
- * deterministic results (no float atomics).  Sums and probabilities are float32.
+ * Conventions: as in moepd.h, on the current device; no state, no allocation, no
+ * synchronisation, and deterministic results (no float atomics).  Sums and probabilities are float32.
  */
 #ifndef MOEPD_BALANCE_H
 #define MOEPD_BALANCE_H

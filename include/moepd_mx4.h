@@ -27,8 +27,8 @@
  * Conventions: as in moepd.h (status codes, borrowed device pointers, host
  * validation before anything is enqueued, no allocation, no synchronisation,
  * a non-null stream; the calls may be captured into a graph).  These calls
- * have no state: any number may run at a time on any streams, and results are
- * deterministic.  Code and scale buffers are 16-byte aligned; other pointers
+ * have no state: any number may run at a time on any streams of the current
+ * device, and results are deterministic.  Code and scale buffers are 16-byte aligned; other pointers
  * need their element's alignment.  Strides are in elements, at least the row's
  * width, or 0 for exactly that.
  */
