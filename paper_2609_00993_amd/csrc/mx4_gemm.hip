@@ -144,7 +144,7 @@ __device__ __forceinline__ float mx4_silu_mul(float g, float u) {
   const float t = -g * kLog2e;
   const float lo = __builtin_fmaf(-g, kLog2e, -t) + -g * kLog2eLow;
   const float e = __builtin_amdgcn_exp2f(t);
-  const float ex = t < 128.f ? __builtin_fmaf(e, lo * kLn2, e) : e;
+  const float ex = __builtin_fabsf(t) < 128.f ? __builtin_fmaf(e, lo * kLn2, e) : e;  // lo of an infinity is NaN
   return g * __builtin_amdgcn_rcpf(1.f + ex) * u;
 }
 

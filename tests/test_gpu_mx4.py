@@ -363,6 +363,27 @@ def test_nan_rows_stay_nan_in_bf16(env, R, N):
         assert bad[R // 2].all() and not np.delete(bad, R // 2, axis=0).any()
 
 
+@pytest.mark.parametrize("R,N", [(3, 64), (300, 512), (700, 4096)])
+@pytest.mark.parametrize("infinite", [False, True])
+def test_gates_past_float32(env, R, N, infinite):
+    """Gates of 1.5 * 2^127 (times log2 e past the largest float) and of infinity are gates like
+    any other: silu of one is itself, and u = 2^-12."""
+    M, torch = env.M, env.torch
+    K = 256
+    codes = np.full((2 * N, K), 2, np.uint8)  # 1.0
+    codes[:N] = 3  # 1.5
+    a = [env.up(h) for h in X.hold(np.full((R, K), 2, np.uint8), np.full((R, K // 32), 127 + 60, np.uint8))]
+    scale = np.full((2 * N, K // 32), 127 - 80, np.uint8)  # u = 2^(8 + 60 - 80)
+    scale[:N] = 127 + 70 if infinite else 127 + 59
+    w = [env.up(h) for h in X.hold(codes, scale)]
+    y = torch.zeros((R, N), device="cuda")
+    torch.cuda.synchronize()
+    env.done(M.moe_mx4_gemm_swiglu(*a, R, *w, 1, None, N, K, y, None, M.MOE_DTYPE_F32, 0, env.s), "product")
+    want = float("inf") if infinite else 1.5 * 2.0 ** (127 - 12)
+    got = y.cpu().numpy().astype(np.float64)
+    assert (got == want).all() if np.isinf(want) else (np.abs(got - want) <= 8 * 2.0 ** -24 * want).all()
+
+
 def test_matrices_past_four_gigabytes(env):
     """Codes, weights and results whose byte offsets pass 32 bits: the last rows are those of a small call."""
     M, torch = env.M, env.torch
