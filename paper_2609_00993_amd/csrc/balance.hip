@@ -246,7 +246,10 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_pieces_kernel(Bala
   for (int first = s < g.S ? seq_begin(g, s) : end; s < g.S && first < end; ++s) {
     const int next = seq_begin(g, s + 1), lo = max(begin, first), hi = min(end, next);
     first = next;
-    if (lo >= hi) continue;  // an empty sequence
+    if (lo >= hi) {  // an empty sequence: past all that follow it at once
+      s = max(s, seq_of(g, max(begin, first)) - 1);
+      continue;
+    }
     add_piece<EPL, BF16>(g, idx, lo, hi, lds);
     uint32_t* slot = slots + (long long)(c + s) * slot_words(g.E);
     for (int e = threadIdx.x; e < g.E; e += 64 * kBalanceWaves) {
@@ -474,8 +477,10 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_backward_kernel(Ba
       const int t = t0 + j;
       if (t >= end) break;
       if (t >= s_end && s < g.S) {
-        while (s < g.S && t >= s_end) {
-          ++s;
+        ++s;
+        if (s < g.S) s_end = seq_begin(g, s + 1);
+        if (s < g.S && t >= s_end) {  // empty sequences: past all of them at once
+          s = max(s, seq_of(g, t));
           if (s < g.S) s_end = seq_begin(g, s + 1);
         }
         s_begin = s < g.S ? seq_begin(g, s) : g.T;

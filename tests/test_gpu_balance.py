@@ -146,6 +146,17 @@ def test_sequences_and_masks(T, E, S):
     _check(clean, idx, None, whole, S, 0.3, Run(clean, idx, None, whole, S))
 
 
+def test_many_empty_sequences():
+    """Runs of thousands of empty sequences, in front, within a chunk, between tokens and at the end."""
+    rng = np.random.default_rng(11)
+    T, E, S = 900, 20, 20000
+    logits = _logits(rng, T, E)
+    idx = _topk(logits, 2)
+    ends = np.sort(rng.choice([0, 1, 7, 8, 9, 300, 640, 641, 899, 900], S - 1)).astype(np.int32)
+    seq = np.concatenate([[0], ends, [T]]).astype(np.int32)
+    _check(logits, idx, None, seq, S, 0.3, Run(logits, idx, None, seq, S))
+
+
 def test_no_live_token():
     rng = np.random.default_rng(2)
     logits, E = _logits(rng, 9, 20), 20
