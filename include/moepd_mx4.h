@@ -85,7 +85,8 @@ int moe_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows
  * with groups = 1: all rows.  Rows of one call are at most `rows`, which also
  * sizes the launch; the tile schedule is read from offsets on the device.
  * k is the width of both matrices (their zero padding is multiplied along).
- * Errors: MOE_ERR_INVALID_ARG, MOE_ERR_HIP. */
+ * Errors: MOE_ERR_INVALID_ARG (also where the launch would take more than 2^31 -
+ * 2^16 workgroups, one for each tile of at least 32 rows and columns), MOE_ERR_HIP. */
 int moe_mx4_gemm(const uint8_t* a, const uint8_t* a_scales, int64_t rows, const uint8_t* w, const uint8_t* w_scales,
                  int32_t groups, const int32_t* offsets, int32_t n, int32_t k, void* out, int32_t out_dtype,
                  int64_t out_stride, hipStream_t stream);

@@ -693,7 +693,7 @@ hipError_t launch_mx4_gemm(Mx4Args g, bool gated, int out, long long expect, hip
     g.n_tiles = (int)((width + bn - 1) / bn + round - 1) / round * round;
     g.run = mean >= 512 ? 64 : 32;
     // row tiles: at most one that is not full for each group that may have a row
-    const long long tiles = (g.rows / bm + (g.groups < g.rows ? g.groups : g.rows)) * g.n_tiles;
+    const long long tiles = ((long long)g.rows / bm + (g.groups < g.rows ? g.groups : g.rows)) * g.n_tiles;
     const long long blocks = round == 8 ? tiles : (tiles + 8 * g.run - 1) / (8 * g.run) * (8 * g.run);  // whole rounds
     if (blocks > 0x7fff0000LL) return hipErrorInvalidValue;
     kernel<<<grid_of(blocks, threads), threads, lds, s>>>(g);

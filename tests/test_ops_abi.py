@@ -122,3 +122,13 @@ def test_balance_backward_refuses(kw):
 
 def test_balance_backward_without_tokens_is_legal():
     assert _call(M.moe_balance_loss_backward, BACK, T=0, logits=None, dlogits=None) == M.MOE_OK
+
+
+@pytest.mark.parametrize("n", [1 << 20, (1 << 20) - 5, 700_001])
+@pytest.mark.parametrize("groups,offsets", [(1, None), (1024, P)])
+def test_products_refuse_more_workgroups_than_a_launch_holds(n, groups, offsets):
+    """Tiles whose number passes 32 bits, multiples of 2^32 among them, are refused, not wrapped."""
+    most = dict(rows=(1 << 31) - 32, n=n, groups=groups, offsets=offsets)
+    for out_dtype in (M.MOE_DTYPE_F32, M.MOE_DTYPE_BF16):
+        assert _call(M.moe_mx4_gemm, GEMM, out_dtype=out_dtype, **most) == BAD
+        assert _call(M.moe_mx4_gemm_swiglu, dict(GEMM, out_scales=None), out_dtype=out_dtype, **most) == BAD
