@@ -42,7 +42,7 @@ extern "C" {
 #endif
 
 /* Limits: rows in [0, 2^31 - 32], cols / n / k in [1, 2^20], groups in
- * [1, 1024], and n x k below 2^33 (n counts gate rows once). */
+ * [1, 1024]. */
 #define MOE_MX4_MAX_COLS (1 << 20)
 #define MOE_MX4_MAX_GROUPS 1024
 
