@@ -136,16 +136,24 @@ __device__ __forceinline__ f32x16_mx4 mx4_mfma(const u32x4& w, const u32x4& a, c
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(w), widen(a), acc, 4, 4, S, (int)sw, S, (int)sa);
 }
 
-// silu(g) * u.  exp(-g) as 2^(t + lo): the product's rounding error and log2 e's
-// own, lo, would otherwise cost |g| ulp; with it, and the hardware's 2^x and
-// reciprocal (1 ulp each), the result is within a few ulp.
+// silu(g) * u.  With q = e^-|g|, silu is g / (1 + q), times q where g is negative: q never
+// overflows, and 1 + q is between 1 and 2.  q as 2^(t + lo): the product's rounding error and
+// log2 e's own, lo, would otherwise cost |g| ulp; with it, and the hardware's 2^x and
+// reciprocal (1 ulp each), the result is within a few ulp.  Far below zero q and g q pass
+// below the normal numbers (which the hardware's 2^x flushes), at -87 and -92, while u may
+// bring the result back: there q carries a factor of 2^64 that 1 + q leaves out and u gives
+// back, good down to gates of -131.  Past 256 q is 0 in any case.
 __device__ __forceinline__ float mx4_silu_mul(float g, float u) {
+#pragma clang fp contract(off)  // t + 64 must start from the rounded t, whose error lo holds
   constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
-  const float t = -g * kLog2e;
-  const float lo = __builtin_fmaf(-g, kLog2e, -t) + -g * kLog2eLow;
-  const float e = __builtin_amdgcn_exp2f(t);
-  const float ex = __builtin_fabsf(t) < 128.f ? __builtin_fmaf(e, lo * kLn2, e) : e;  // lo of an infinity is NaN
-  return g * __builtin_amdgcn_rcpf(1.f + ex) * u;
+  const float a = fminf(__builtin_fabsf(g), 256.f);
+  const float t = -a * kLog2e;
+  const float lo = __builtin_fmaf(-a, kLog2eLow, __builtin_fmaf(-a, kLog2e, -t));
+  const bool deep = g < -44.f;
+  const float k = deep ? 0x1p-64f : 1.f;
+  const float e = __builtin_amdgcn_exp2f(t + (deep ? 64.f : 0.f));
+  const float q = __builtin_fmaf(e, lo * kLn2, e);
+  return (g < 0.f ? g * q : g) * __builtin_amdgcn_rcpf(__builtin_fmaf(q, k, 1.f)) * (u * k);
 }
 
 // Two values to bf16, nearest even, packed.

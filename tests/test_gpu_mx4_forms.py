@@ -28,3 +28,43 @@ def test_one_matrix_of_2_to_the_34_weights(env, R):
     want, mag = X.product(av, X.dequantize(*(v[:, :n] for v, n in zip(X.release(*ends, last, K), (K, K // 32)))), [0, R], last)
     assert (np.abs(y[:, N - last:].cpu().numpy() - want) <= _sum_bound(mag, K)).all()
     assert bool((y[:, ::4099] != 0).any(dim=0).all())
+
+
+def _gate_codes(value):
+    """Codes of at most 32 magnitudes of E2M1 that add up to `value`, a multiple of 0.5."""
+    codes, left = [], value
+    for code, mag in ((7, 6.0), (6, 4.0), (5, 3.0), (4, 2.0), (3, 1.5), (2, 1.0), (1, 0.5)):
+        while left >= mag:
+            codes.append(code)
+            left -= mag
+    assert left == 0 and len(codes) <= 32
+    return codes
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("R,N", [(3, 256), (40, 512), (700, 4096)])
+def test_gates_far_below_zero(env, R, N, out):
+    """silu(gate) * up where e^gate, then silu(gate) itself, pass below float32's normal numbers and
+    up brings the product back: 16 u for its evaluation, and no more, down to gates of -110."""
+    M, torch = env.M, env.torch
+    K, up = 256, 2.0 ** 100
+    gates = -0.5 * (np.arange(N) % 221)
+    codes = np.zeros((2 * N, K), np.uint8)
+    for c, g in enumerate(gates):
+        q = _gate_codes(-g)
+        codes[c, :len(q)] = np.array(q, np.uint8) | 8
+    codes[N:, 64] = 2  # 1.0
+    scales = np.full((2 * N, K // 32), 127, np.uint8)
+    scales[N:, 2] = 127 + 100
+    a = [env.up(h) for h in X.hold(np.full((R, K), 2, np.uint8), np.full((R, K // 32), 127, np.uint8))]
+    w = [env.up(h) for h in X.hold(codes, scales)]
+    code, dtype = env.types[out]
+    y = torch.zeros((R, N), dtype=dtype, device="cuda")
+    torch.cuda.synchronize()
+    env.done(M.moe_mx4_gemm_swiglu(*a, R, *w, 1, None, N, K, y, None, code, 0, env.s), "product")
+    want = X.swiglu(gates, np.full(N, up))
+    bound = 16 * 2.0 ** -24 * np.abs(want) + 2.0 ** -140
+    if out == "bf16":
+        bound = bound + 2.0 ** -8 * (np.abs(want) + bound)
+    err = np.abs(y.float().cpu().numpy().astype(np.float64) - want)
+    assert (err <= bound).all(), sorted(set(gates[np.argwhere(err > bound)[:, 1]]))
