@@ -15,13 +15,9 @@
 #pragma once
 
 #include "common.h"
+#include "mx4_form.h"
 
 namespace moepd {
-
-constexpr int kMx4Rows = 32;    // rows of a held block
-constexpr int kMx4Slice = 256;  // K values that share scale words; the padding of K
-constexpr int kMx4SliceBytes = 4096;  // codes of 32 rows x 256 values
-constexpr int kMx4SliceScales = 256;  // their scales
 
 __host__ __device__ inline int mx4_slices(int cols) { return (cols + kMx4Slice - 1) / kMx4Slice; }
 

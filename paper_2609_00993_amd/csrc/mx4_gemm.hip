@@ -221,11 +221,10 @@ __device__ __forceinline__ void mx4_store(const Mx4Args& g, const float (&v)[16]
 
 // A lane's place in a run of rows of a held matrix: its code bytes and scale bytes
 // from the block of the run's first row, or past every resource where the row does
-// not count (such loads give zeros and touch no memory).
+// not count (kMx4Nowhere: such loads give zeros and touch no memory).
 struct Mx4Lane {
   int codes, scales;
 };
-constexpr int kMx4Nowhere = 0x7fffff00;
 __device__ __forceinline__ Mx4Lane mx4_lane(long long first, int row, bool counts, int slices, int h) {
   const int rr = (int)(first & 31) + row;
   const int b = rr >> 5, r = rr & 31;
@@ -303,7 +302,7 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
                                                      at * kMx4SliceScales, 0);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        s.w[j][i] = mx4_load(w_span[j].rsrc(in ? w_span[j].bytes : 0), wl[j].codes + i * 1024, at * kMx4SliceBytes);
+        s.w[j][i] = mx4_load(w_span[j].rsrc(in ? w_span[j].bytes : 0), wl[j].codes + i * kMx4StepBytes, at * kMx4SliceBytes);
     }
 #pragma unroll
     for (int m = 0; m < MB; ++m) {
@@ -311,7 +310,7 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
                                                      at * kMx4SliceScales, 0);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        s.a[m][i] = mx4_load(a_span.rsrc(in ? a_span.bytes : 0), al[m].codes + i * 1024, at * kMx4SliceBytes);
+        s.a[m][i] = mx4_load(a_span.rsrc(in ? a_span.bytes : 0), al[m].codes + i * kMx4StepBytes, at * kMx4SliceBytes);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -506,8 +505,8 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
   Mx4Span w_span[2], ws_span[2];
   // Row block b is MB - 1 blocks at most past the first; only the last one may be cut short.
   Mx4Lane full = mx4_lane(m0, r, true, KT, h), cut = mx4_lane(m0, r, 32 * (MB - 1) + r < m_rows, KT, h);
-  full.codes += wave * 1024;  // of a slice of `a`, this wave moves step `wave`
-  cut.codes += wave * 1024;
+  full.codes += wave * kMx4StepBytes;  // of a slice of `a`, this wave moves step `wave`
+  cut.codes += wave * kMx4StepBytes;
   Mx4Lane wl[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -544,7 +543,7 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
                                              a_slice * kMx4SliceBytes, 0, 0);
   };
   auto load_w = [&](int j, int s, int p) {
-    wf[p][j][s] = mx4_load(w_span[j].rsrc(w_in ? w_span[j].bytes : 0), wl[j].codes + s * 1024, w_slice * kMx4SliceBytes);
+    wf[p][j][s] = mx4_load(w_span[j].rsrc(w_in ? w_span[j].bytes : 0), wl[j].codes + s * kMx4StepBytes, w_slice * kMx4SliceBytes);
   };
   auto load_sw = [&](int j, int p) {
     sw[p][j] = __builtin_amdgcn_raw_buffer_load_b32(ws_span[j].rsrc(w_in ? ws_span[j].bytes : 0), wl[j].scales,
@@ -672,7 +671,6 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
 // share a CU: one's start and end, which take as long as eight slices, run beside the
 // other's slices (256-row tiles, one to a CU, took 150 us where these take 103: 8192 rows
 // over 32 groups, 7168 x 2048).
-constexpr int kRingSlots = 3, kRingBlocks = 4;
 template <bool GATED, int OUT>
 __global__ __launch_bounds__(256, 2) void mx4_ring_kernel(Mx4Args g) {
   constexpr int ring = kRingSlots * kRingBlocks * 256, parts = 4 * Mx4Patch<OUT, GATED ? 32 : 64>::bytes / 16;
