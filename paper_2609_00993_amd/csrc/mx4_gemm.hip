@@ -397,7 +397,6 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
 
 // Tiles of up to 32 MAXB rows: 32 where groups are expected to have few rows, since without
 // the 64-row body the kernel takes registers for three waves to a SIMD instead of two.
-constexpr int kStreamWaves = 8;
 template <int MAXB, int NB, bool GATED, int OUT>
 __global__ __launch_bounds__(64 * kStreamWaves, MAXB == 2 ? 2 : NB == 2 ? 3 : 4) void mx4_stream_kernel(
     Mx4Args g) {
@@ -685,53 +684,26 @@ __global__ __launch_bounds__(256, 2) void mx4_ring_kernel(Mx4Args g) {
   });
 }
 
-inline int up8(long long v) { return (int)((v + 7) / 8 * 8); }
-
 }  // namespace
 
 hipError_t launch_mx4_gemm(Mx4Args g, bool gated, int out, long long expect, hipStream_t s) {
   const long long width = out == kMx4Fp4 ? (g.n + kMx4Slice - 1) / kMx4Slice * kMx4Slice : g.n;
-  if (expect < 1) expect = 1;
-  if (expect > g.rows) expect = g.rows;
-  const long long touched = g.groups < expect ? g.groups : expect;  // groups that have a row
-  const int mean = (int)(expect / touched);
-  auto launch = [&](auto kernel, int bm, int bn, int threads, size_t lds, int round) {
-    g.n_tiles = (int)((width + bn - 1) / bn + round - 1) / round * round;
-    g.run = mean >= 512 ? 64 : 32;
-    // row tiles: at most one that is not full for each group that may have a row
-    const long long tiles = ((long long)g.rows / bm + (g.groups < g.rows ? g.groups : g.rows)) * g.n_tiles;
-    const long long blocks = round == 8 ? tiles : (tiles + 8 * g.run - 1) / (8 * g.run) * (8 * g.run);  // whole rounds
-    if (blocks > 0x7fff0000LL) return hipErrorInvalidValue;
-    kernel<<<grid_of(blocks, threads), threads, lds, s>>>(g);
+  const Mx4Form f = mx4_form(gated, width, g.rows, g.groups, g.slices, expect < 1 ? 1 : expect < g.rows ? expect : g.rows);
+  if (!f.fits()) return hipErrorInvalidValue;
+  g.n_tiles = f.n_tiles;
+  g.run = f.run;
+  auto launch = [&](auto kernel) {
+    kernel<<<grid_of(f.groups, f.threads()), f.threads(), f.lds(), s>>>(g);
     return hipGetLastError();
   };
-  // Expected tiles of bm rows and bn columns.
-  auto tiles_of = [&](int bm, int bn) { return (width + bn - 1) / bn * (expect / bm + touched); };
-  // Streaming tiles: waves to share a tile, enough to keep the memory busy, 8 to a CU.
-  auto stream = [&](auto kernel, int bm, int bn, int panels) {
-    int waves = 1;
-    while (waves < kStreamWaves && tiles_of(bm, bn) * waves < 8 * 256 && waves * 2 <= g.slices) waves *= 2;
-    return launch(kernel, bm, bn, 64 * waves, waves > 1 ? (size_t)waves * (bm / 32) * panels * 4096 : 0, 8);
-  };
-  // Ring tiles from 16 rows a group on (32 gated), if there are enough for many CUs.  us, ring / streaming tiles: 18
-  // rows in each of 64 groups, 2560 x 768, 18.4 / 19.3; 20 in each of 32, 7168 x 2048, 41.8 / 42.9, and
-  // gated, 2048 x 7168, 89.7 / 88.0; 28 in each of 64, gated, 768 x 2560, 31.4 / 29.0.  One matrix of
-  // 7168 x 7168: 128 rows (28 ring tiles) 28.6 / 18.2, 256 (56) 28.1 / 22.2, 512 (112) 28.6 / 36.1.
   auto go = [&](auto gate, auto kind) {
     constexpr bool GATED = decltype(gate)::value;
     constexpr int OUT = decltype(kind)::value;
-    if (mean >= (GATED ? 32 : 16) && tiles_of(128, GATED ? 128 : 256) >= 100)
-      return launch(mx4_ring_kernel<GATED, OUT>, 128, GATED ? 128 : 256, 256, 0, 1);
-    const bool tall = mean > 32;
-    if constexpr (GATED) {
-      return tall ? stream(mx4_stream_kernel<2, 2, true, OUT>, 64, 32, 2) : stream(mx4_stream_kernel<1, 2, true, OUT>, 32, 32, 2);
-    } else {
-      // panels of 32 columns where those of 64 would leave CUs idle
-      const bool narrow = tiles_of(tall ? 64 : 32, 64) < 256;
-      if (tall)
-        return narrow ? stream(mx4_stream_kernel<2, 1, false, OUT>, 64, 32, 1) : stream(mx4_stream_kernel<2, 2, false, OUT>, 64, 64, 2);
-      return narrow ? stream(mx4_stream_kernel<1, 1, false, OUT>, 32, 32, 1) : stream(mx4_stream_kernel<1, 2, false, OUT>, 32, 64, 2);
+    if (f.ring) return launch(mx4_ring_kernel<GATED, OUT>);
+    if constexpr (!GATED) {
+      if (f.panels == 1) return f.blocks == 2 ? launch(mx4_stream_kernel<2, 1, false, OUT>) : launch(mx4_stream_kernel<1, 1, false, OUT>);
     }
+    return f.blocks == 2 ? launch(mx4_stream_kernel<2, 2, GATED, OUT>) : launch(mx4_stream_kernel<1, 2, GATED, OUT>);
   };
   using Plain = std::false_type;
   using Gated = std::true_type;

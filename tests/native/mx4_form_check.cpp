@@ -3,14 +3,23 @@
 // Without arguments: checks, in 64 bits, that the byte offsets a lane forms stay within
 // 31 bits whatever the matrix's width, that those of a row which counts lie within its
 // tile's resource, and that those of a row which does not lie past every resource.
+// With "form gated width rows groups slices expect": prints the form of a launch.
 #include <cstdio>
+#include <cstdlib>
+#include <cstring>
 #include <initializer_list>
 
 #include "mx4_form.h"
 
 using namespace moepd;
 
-int main() {
+int main(int argc, char** argv) {
+  if (argc == 8 && !std::strcmp(argv[1], "form")) {
+    const Mx4Form f = mx4_form(std::atoi(argv[2]), std::atoll(argv[3]), std::atoll(argv[4]), std::atoi(argv[5]),
+                               std::atoi(argv[6]), std::atoll(argv[7]));
+    std::printf("%d %d %d %d\n", f.ring, f.blocks, f.panels, f.waves);
+    return 0;
+  }
   int bad = 0;
   auto check = [&](const char* what, bool holds, int slices, int block, long long at) {
     if (holds) return;

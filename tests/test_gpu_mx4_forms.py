@@ -1,11 +1,13 @@
 """MX FP4 products on the GPU in each form of their tiles, and where sizes, gates and
 scales are extreme.  Bounds are those of tests/test_gpu_mx4.py."""
 
+from typing import NamedTuple, Optional
+
 import numpy as np
 import pytest
 
 from oracle import mx4 as X
-from tests.test_gpu_mx4 import _matrix, _need_gpu, _sum_bound, env  # noqa: F401
+from tests.test_gpu_mx4 import _gated, _matrix, _need_gpu, _run_product, _sum_bound, env  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -68,3 +70,109 @@ def test_gates_far_below_zero(env, R, N, out):
         bound = bound + 2.0 ** -8 * (np.abs(want) + bound)
     err = np.abs(y.float().cpu().numpy().astype(np.float64) - want)
     assert (err <= bound).all(), sorted(set(gates[np.argwhere(err > bound)[:, 1]]))
+
+
+class Case(NamedTuple):
+    """A product whose launch takes the form it is listed for (tests/test_mx4_form.py holds that
+    without a GPU)."""
+
+    name: str
+    groups: Optional[tuple]  # rows of each group; None: one matrix of all rows
+    rows: int
+    N: int
+    K: int
+    gated: bool
+    out: str
+    before: int = 0  # rows of no group in front
+    stride: int = 0  # 0: N
+    pad: int = 0
+    clamp: bool = False  # the last offset lies past the rows
+
+    @property
+    def offsets(self):
+        if self.groups is None:
+            return None
+        o = self.before + np.concatenate([[0], np.cumsum(self.groups)])
+        assert o[-1] <= self.rows
+        if self.clamp:
+            o[-1] = self.rows + 1000
+        return o
+
+    @property
+    def group_rows(self):
+        return (self.rows,) if self.groups is None else tuple(np.diff(np.clip(self.offsets, 0, self.rows)).tolist())
+
+
+# rows of a group at the edges of 32-row blocks and of 128-row tiles, cut in one, two, three and four
+EDGES = (1, 31, 32, 33, 0, 63, 64, 65, 96, 97, 127, 128, 129, 160, 200, 255, 256, 257, 320, 385)
+KINDS = [(False, "f32"), (False, "bf16"), (True, "f32"), (True, "bf16"), (True, "fp4")]
+
+
+def _cases():
+    for gated, out in KINDS:
+        tag = f"{'gated' if gated else 'plain'}-{out}"
+        odd = out != "fp4"  # MX FP4 rows are whole blocks
+        # ring tiles: one to seven slices, so the ring goes round, ends at either parity and in every slot
+        n = (289 if odd else 288) if gated else 577
+        for i, K in enumerate((200, 512, 700, 1000, 1270, 1700)):
+            yield Case(f"ring-{tag}-K{K}", EDGES, sum(EDGES) + 9, n, K, gated, out, before=5,
+                       stride=(0, n + 1, n + 6)[i % 3] * odd, pad=(0, 1, 3)[i // 2] * odd, clamp=i % 2 == 1)
+        # groups found in the second and third run of 64
+        many = tuple(20 + 25 * gated + (7 * g) % 11 for g in range(140))
+        yield Case(f"ring-{tag}-140-groups", many, sum(many), 40 if odd else 64, 600, gated, out)
+        # one group has all the rows; one matrix, its last column tile cut
+        yield Case(f"ring-{tag}-one-group", (0, 2900, 0), 2950, (2 - gated) * 513 if odd else 544, 768, gated, out, before=20)
+        yield Case(f"ring-{tag}-dense", None, 417, 3333 * (2 - gated) if odd else 3360, 760, gated, out)
+        # streaming tiles: a tile's slices shared by one to eight waves, and dealt unevenly
+        for rows in (7, 20, 32):
+            yield Case(f"stream-{tag}-{rows}", None, rows, 1001 if odd else 992, (256, 700, 2300)[rows % 3], gated, out,
+                       stride=1004 * odd, pad=odd)
+        yield Case(f"stream-{tag}-few-groups", (3, 0, 9, 1, 32, 33, 40), 125, 201 if odd else 192, 1270, gated, out, before=4)
+        yield Case(f"stream-{tag}-wide", tuple(1 + g % 15 for g in range(40)), 320, (161 if odd else 160) if gated else 481,
+                   1270, gated, out, before=2, clamp=True)
+        yield Case(f"stream-{tag}-tall", None, 70, 1001 if odd else 992, 2300, gated, out)
+        yield Case(f"stream-{tag}-tall-wide", None, 1000 if not gated else 260, 1501 if odd else 1504, 1400, gated, out,
+                   stride=1504 * odd, pad=odd)
+        yield Case(f"stream-{tag}-tall-groups", (33, 70, 64, 0, 129, 65, 1), 370, 490 if odd else 480, 600, gated, out)
+    for gated in (False, True):  # enough tiles for one wave each, several slices
+        many = tuple((14 + 12 * gated) - g % 2 for g in range(200))
+        yield Case(f"stream-{'gated' if gated else 'plain'}-one-wave", many, sum(many) + 30, 193 if gated else 520, 513, gated,
+                   "f32", before=30)
+        yield Case(f"stream-{'gated' if gated else 'plain'}-tall-one-wave", None, 70, 1001, 250, gated, "f32")
+
+
+CASES = list(_cases())
+
+
+@pytest.mark.parametrize("case", CASES, ids=[c.name for c in CASES])
+def test_products_in_every_form(env, case):
+    c = case
+    rng = np.random.default_rng(CASES.index(c) + 1)
+    if c.out != "fp4":
+        _run_product(env, rng, c.rows, c.N, c.K, c.offsets, c.gated, c.out, c.stride or c.N, c.pad)
+        return
+    M = env.M
+    offs = [0, c.rows] if c.groups is None else c.offsets
+    a, av = _matrix(env, rng, c.rows, c.K, 2)
+    w, wv = _matrix(env, rng, (len(offs) - 1) * 2 * c.N, c.K, 2)
+    h = env.matrix(c.rows, c.N)
+    dev = None if c.groups is None else env.up(np.array(offs, np.int32))
+    env.done(M.moe_mx4_gemm_swiglu(*a, c.rows, *w, len(offs) - 1, dev, c.N, c.K, *h, M.MOE_DTYPE_FP4, 0, env.s), "swiglu")
+    y, mag = X.product(av, wv, np.clip(offs, 0, c.rows), 2 * c.N)
+    ref, bound = _gated(y, _sum_bound(mag, c.K), c.N)
+    codes, scales = X.release(h[0].cpu().numpy(), h[1].cpu().numpy(), c.rows, c.N)
+    mine = ~np.isnan(ref[:, 0])
+    assert (codes[~mine] == [[5]]).sum() == codes[~mine][:, 0::2].size and (scales[~mine] == 0xA5).all()  # 0xA5 as it was
+    assert not (codes[mine, c.N:] & 7).any() and not scales[mine, c.N // 32:].any()  # the padding is zeros
+    ref, bound, codes, scales = ref[mine], bound[mine], codes[mine, :c.N], scales[mine, :c.N // 32]
+
+    def byte(v):
+        return np.clip(np.floor(np.log2(np.maximum(v, 1e-300))) - 2 + 127, 0, 254)
+
+    lo = np.maximum(np.abs(ref) - bound, 0).reshape(len(ref), -1, 32).max(axis=2)
+    hi = (np.abs(ref) + bound).reshape(len(ref), -1, 32).max(axis=2)
+    assert (scales >= byte(lo)).all() and (scales <= byte(hi)).all()
+    scale = np.repeat(np.exp2(scales.astype(np.float64) - 127), 32, axis=1)
+    got = X.dequantize(codes, scales)
+    assert (got >= X.e2m1_decode(X.e2m1_encode((ref - bound) / scale)) * scale).all()
+    assert (got <= X.e2m1_decode(X.e2m1_encode((ref + bound) / scale)) * scale).all()
