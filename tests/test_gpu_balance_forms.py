@@ -1,0 +1,60 @@
+"""The balance loss and gradient on the GPU in each form of their kernels, by the bounds of
+tests/test_gpu_balance.py."""
+
+import numpy as np
+import pytest
+
+from tests.test_gpu_balance import Run, _check, _logits, _need_gpu, _topk  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# One launch does it all up to 256 tokens x 64 experts of one sequence: the last shape of
+# each count of experts to a lane that takes it, and the first that does not.
+EDGES = [(256, 64, 4), (257, 64, 4), (128, 128, 8), (129, 127, 8), (85, 192, 2), (86, 192, 2), (64, 253, 8), (65, 256, 8),
+         (51, 300, 16), (52, 300, 16), (32, 512, 8), (33, 511, 8), (28, 570, 1), (29, 570, 1), (16, 1000, 3), (16, 1024, 16),
+         (17, 1024, 16), (1, 513, 4), (1, 1024, 8)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,E,k", EDGES)
+def test_one_launch_and_its_edges(T, E, k, dtype):
+    rng = np.random.default_rng(T * 1031 + E)
+    logits = _logits(rng, T, E, dtype)
+    idx = _topk(logits, k)
+    _check(logits, idx, None, None, 1, 0.3, Run(logits, idx, dtype=dtype), dtype)
+    # one sequence that leaves tokens out at both ends, some masked
+    seq = np.array([T // 8, T - T // 5], np.int32)
+    mask = (rng.random(T) < 0.7).astype(np.uint8)
+    _check(logits, idx, mask, seq, 1, 0.3, Run(logits, idx, mask, seq, 1, dtype=dtype, stride=E + 5), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("E", [129, 250, 300, 513, 1023])
+def test_padded_rows_accumulate_and_in_place_at_four_experts_to_a_lane(E, dtype):
+    rng = np.random.default_rng(E)
+    T = 61
+    logits = _logits(rng, T, E, dtype)
+    idx = _topk(logits, 6)
+    seq = np.array([1, 20, 20, 55], np.int32)
+    mask = (rng.random(T) < 0.8).astype(np.uint8)
+    base = _logits(rng, T, E, dtype, 1e-3)
+    grad = np.array([-2.5], np.float32)
+    for stride in (E, E + 1, E + 4 - E % 4, E + 6):
+        for kw in (dict(grad=grad), dict(grad=grad, base=base), dict(grad=grad, inplace=True)):
+            _check(logits, idx, mask, seq, 3, 0.3, Run(logits, idx, mask, seq, 3, stride=stride, dtype=dtype, **kw), dtype, -2.5,
+                   kw.get("base"))
+
+
+@pytest.mark.parametrize("T,E,S,long", [(3000, 100, 100, 1), (2600, 256, 60, 1), (5000, 64, 1100, 1), (4000, 200, 1500, 2),
+                                        (700, 33, 5000, 1)])
+def test_long_sequences_among_single_tokens(T, E, S, long):
+    """`long` sequences hold nearly all the tokens, between runs of sequences of one token and of none."""
+    rng = np.random.default_rng(S)
+    logits = _logits(rng, T, E)
+    idx = _topk(logits, 3)
+    sizes = rng.integers(0, 2, S)
+    at = rng.choice(S, long, replace=False)
+    sizes[at] = (T - sizes.sum() + sizes[at].sum()) // long if sizes.sum() < T else 0
+    ends = np.minimum(np.cumsum(sizes), T)
+    seq = np.concatenate([[0], ends]).astype(np.int32)
+    _check(logits, idx, None, seq, S, 0.3, Run(logits, idx, None, seq, S))
