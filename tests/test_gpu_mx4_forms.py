@@ -176,3 +176,78 @@ def test_products_in_every_form(env, case):
     got = X.dequantize(codes, scales)
     assert (got >= X.e2m1_decode(X.e2m1_encode((ref - bound) / scale)) * scale).all()
     assert (got <= X.e2m1_decode(X.e2m1_encode((ref + bound) / scale)) * scale).all()
+
+
+def _low_rows(dtype):
+    """Blocks whose largest magnitudes run from 2^-149 (bf16: 2^-133) up past the smallest block
+    exponents, each with every code, the ties between codes and their neighbours, and both signs."""
+    least = -149 if dtype == "f32" else -133
+    mults = np.array([0, 0.25, 0.5, 0.75, 1, 1.25, 1.5, 1.75, 2, 2.5, 3, 3.5, 4, 5, 6, 7], np.float64)
+    rows = []
+    for e in range(least, -113):
+        v = np.concatenate([mults, -mults]) * 2.0 ** e  # largest 7 * 2^e: the block's exponent is e, or -127
+        w = v.copy()
+        w[np.abs(w) > 4 * 2.0 ** e] /= 4.0  # the same with a largest magnitude of 4 * 2^e
+        f = np.float32 if dtype == "f32" else None
+        for r in (v, w):
+            r32 = r.astype(np.float32)  # rounds what float32 cannot hold
+            if f is None:
+                r32 = (r32.view(np.uint32) >> 16 << 16).view(np.float32)
+            rows.append(r32)
+    return np.stack(rows)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_smallest_block_exponents_are_exact(env, dtype):
+    """Scale bytes 0, 1, 2 ... with every code, subnormal inputs and subnormal values: exact both ways."""
+    M, torch = env.M, env.torch
+    v = _low_rows(dtype)
+    R, K = v.shape
+    codes, scales = X.quantize(v)
+    # byte 0 and its neighbours carry every code (of byte 0: all eight magnitudes, from subnormal inputs alone too)
+    for byte in (0, 1, 2, 3):
+        assert set((codes[scales[:, 0] == byte] & 7).ravel().tolist()) == set(range(8)), byte
+    code, t = env.types[dtype]
+    x = torch.from_numpy(v).cuda().to(t)
+    held = env.matrix(R, K)
+    torch.cuda.synchronize()
+    assert np.array_equal(x.float().cpu().numpy(), v)
+    env.done(M.moe_mx4_quantize(x, code, 0, R, K, None, None, *held, env.s), "quantize")
+    c, s = X.release(held[0].cpu().numpy(), held[1].cpu().numpy(), R, K)
+    assert np.array_equal(s[:, :1], scales)
+    same = (c[:, :K] == codes) | ((c[:, :K] & 7) + (codes & 7) == 0)
+    assert same.all(), np.argwhere(~same)[:5]
+    want = X.dequantize(codes, scales)
+    for name, (out_code, out_t) in env.types.items():
+        out = torch.full((R, K), float("nan"), dtype=out_t, device="cuda")
+        torch.cuda.synchronize()
+        env.done(M.moe_mx4_dequantize(*held, R, K, out, out_code, 0, env.s), "dequantize")
+        assert np.array_equal(out.float().cpu().numpy().astype(np.float64), want), name
+
+
+@pytest.mark.parametrize("R,N", [(40, 70), (700, 4100)])
+def test_products_of_the_smallest_and_largest_scales(env, R, N):
+    """Rows of scale bytes 0 to 3 times weights of bytes 214 to 254: within the bound, not flushed."""
+    M, torch = env.M, env.torch
+    rng = np.random.default_rng(R)
+    K = 512
+    codes = rng.integers(0, 16, (R, K), dtype=np.uint8)
+    scales = rng.integers(0, 4, (R, K // 32), dtype=np.uint8)
+    wcodes = rng.integers(0, 16, (N, K), dtype=np.uint8)
+    wscales = np.repeat(rng.integers(214, 251, (N, 1), dtype=np.uint8), K // 32, axis=1) + rng.integers(0, 5, (N, K // 32), dtype=np.uint8)
+    y, mag = X.product(X.dequantize(codes, scales), X.dequantize(wcodes, wscales), [0, R], N)
+    a, w = ([env.up(h) for h in X.hold(*m)] for m in ((codes, scales), (wcodes, wscales)))
+    out = torch.zeros((R, N), device="cuda")
+    torch.cuda.synchronize()
+    env.done(M.moe_mx4_gemm(*a, R, *w, 1, None, N, K, out, M.MOE_DTYPE_F32, 0, env.s), "gemm")
+    assert (np.abs(out.cpu().numpy() - y) <= _sum_bound(mag, K)).all()
+    # and the other way about
+    out.zero_()
+    torch.cuda.synchronize()
+    y, mag = X.product(X.dequantize(wcodes, wscales)[:R], X.dequantize(codes, scales)[:N], [0, min(R, N)], min(R, N))
+    n = min(R, N)
+    a, w = ([env.up(h) for h in X.hold(*m)] for m in ((wcodes[:n], wscales[:n]), (codes[:n], scales[:n])))
+    out = torch.zeros((n, n), device="cuda")
+    torch.cuda.synchronize()
+    env.done(M.moe_mx4_gemm(*a, n, *w, 1, None, n, K, out, M.MOE_DTYPE_F32, 0, env.s), "gemm")
+    assert (np.abs(out.cpu().numpy() - y[:n]) <= _sum_bound(mag[:n], K)).all()
