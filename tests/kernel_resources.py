@@ -35,8 +35,8 @@ def _code_objects():
         at = data.find(MAGIC, at + 1)
 
 
-def kernels():
-    """{demangled kernel name: (VGPRs with AGPRs as allocated, LDS bytes)}."""
+def resources():
+    """{demangled kernel name: the metadata's numbers}."""
     got = {}
     for elf in _code_objects():
         with tempfile.NamedTemporaryFile(suffix=".co") as f:
@@ -45,9 +45,12 @@ def kernels():
             notes = subprocess.run([READELF, "--notes", f.name], stdout=subprocess.PIPE, text=True, check=True).stdout
         for block in re.split(r"\n  - \.agpr_count:", notes)[1:]:
             name = re.search(r"\.name: +(\S+)", block).group(1)
-            vgprs = int(re.search(r"\.vgpr_count: +(\d+)", block).group(1))
-            lds = int(re.search(r"\.group_segment_fixed_size: +(\d+)", block).group(1))
-            got[name] = (-(-vgprs // VGPR_UNIT) * VGPR_UNIT, lds)
+            got[name] = {k: int(v) for k, v in re.findall(r"\n    \.(\w+): +(\d+)(?=\n)", block)}
     names = subprocess.run(["c++filt"], input="\n".join(got), stdout=subprocess.PIPE, text=True, check=True).stdout
-    return dict(zip((n.split("(")[0].replace("moepd::", "").replace("void ", "") for n in names.split("\n")),
-                    got.values()))
+    names = (n.replace("(anonymous namespace)::", "").split("(")[0] for n in names.split("\n"))
+    return dict(zip((n.replace("moepd::", "").replace("void ", "") for n in names), got.values()))
+
+
+def kernels():
+    """{demangled kernel name: (VGPRs with AGPRs as allocated, LDS bytes)}."""
+    return {n: (-(-r["vgpr_count"] // VGPR_UNIT) * VGPR_UNIT, r["group_segment_fixed_size"]) for n, r in resources().items()}
