@@ -58,3 +58,51 @@ def test_long_sequences_among_single_tokens(T, E, S, long):
     ends = np.minimum(np.cumsum(sizes), T)
     seq = np.concatenate([[0], ends]).astype(np.int32)
     _check(logits, idx, None, seq, S, 0.3, Run(logits, idx, None, seq, S))
+
+
+@pytest.mark.parametrize("T,E,S", [(40, 60, 1), (3000, 130, 1), (3000, 130, 9), (900, 200, 1200)])
+def test_a_captured_loss_and_gradient_replay(T, E, S):
+    """The one-launch form, the join that ends with a ticket and the join of its own for many sequences,
+    captured once: replays on new logits, with eager calls between, give the eager bits."""
+    import torch
+
+    from paper_2609_00993_amd import moepd as M
+
+    rng = np.random.default_rng(T + S)
+    k, s = 4, torch.cuda.Stream()
+    seq = None
+    if S > 1:
+        seq = torch.from_numpy(np.concatenate([[0], np.sort(rng.integers(0, T + 1, S - 1)), [T]]).astype(np.int32)).cuda()
+    x, idx = torch.zeros((T, E), device="cuda"), torch.zeros((T, k), dtype=torch.int32, device="cuda")
+    st, n = M.moe_balance_workspace(T, E, S)
+    M.check(st)
+
+    def outputs():
+        return [torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.zeros(1, device="cuda"),
+                torch.zeros((S, E), dtype=torch.int32, device="cuda"), torch.zeros(S + 1, dtype=torch.int32, device="cuda"),
+                torch.zeros((T, E), device="cuda")]
+
+    def call(ws, loss, counts, live, d):
+        M.check(M.moe_balance_loss(x, M.MOE_DTYPE_F32, 0, idx, None, seq, S, T, E, k, 0.3, loss, counts, live, ws, n, s))
+        M.check(M.moe_balance_loss_backward(x, M.MOE_DTYPE_F32, 0, None, seq, S, T, E, k, 0.3, counts, live, None, d, 0, False, s))
+
+    mine, eager = outputs(), outputs()
+    torch.cuda.synchronize()
+    call(*eager)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        call(*mine)
+    for _ in range(4):
+        logits = _logits(rng, T, E)
+        x.copy_(torch.from_numpy(logits))
+        idx.copy_(torch.from_numpy(_topk(logits, k)))
+        for t in mine:
+            t.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        call(*eager)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(mine[1:], eager[1:]))
+        assert float(mine[1]) > 0 and int(mine[3][S]) > 0
