@@ -106,3 +106,40 @@ def test_a_captured_loss_and_gradient_replay(T, E, S):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(mine[1:], eager[1:]))
         assert float(mine[1]) > 0 and int(mine[3][S]) > 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_whose_offsets_pass_32_bits(dtype):
+    """Logits and gradients 2^20 elements and more a row: the last rows lie past 2^32 elements."""
+    import torch
+
+    from paper_2609_00993_amd import moepd as M
+
+    rng = np.random.default_rng(12)
+    T, E, k, stride = 4200, 130, 4, (1 << 20) + 3
+    logits = _logits(rng, T, E, dtype)
+    idx = _topk(logits, k)
+    s, t = torch.cuda.Stream(), torch.float32 if dtype == "f32" else torch.bfloat16
+    code = M.MOE_DTYPE_F32 if dtype == "f32" else M.MOE_DTYPE_BF16
+    assert (T - 1) * stride > 1 << 32
+    x, d = (torch.empty(T * stride, dtype=t, device="cuda").view(T, stride) for _ in range(2))
+    x[:, :E] = torch.from_numpy(logits).cuda().to(t)
+    x[:, E], d[:, E] = float("nan"), float("nan")
+    i = torch.from_numpy(idx).cuda()
+    st, n = M.moe_balance_workspace(T, E, 1)
+    M.check(st)
+    ws, loss = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.zeros(1, device="cuda")
+    counts, live = torch.zeros((1, E), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    M.check(M.moe_balance_loss(x, code, stride, i, None, None, 1, T, E, k, 0.3, loss, counts, live, ws, n, s))
+    M.check(M.moe_balance_loss_backward(x, code, stride, None, None, 1, T, E, k, 0.3, counts, live, None, d, stride, False, s))
+    torch.cuda.synchronize()
+
+    class Got:
+        pass
+
+    got = Got()
+    got.loss, got.counts, got.live = float(loss), counts.cpu().numpy(), live.cpu().numpy()
+    got.d = d[:, :E].float().cpu().numpy().astype(np.float64)
+    assert bool(torch.isnan(d[:, E]).all())
+    _check(logits, idx, None, None, 1, 0.3, got, dtype)

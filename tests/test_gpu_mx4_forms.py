@@ -251,3 +251,36 @@ def test_products_of_the_smallest_and_largest_scales(env, R, N):
     torch.cuda.synchronize()
     env.done(M.moe_mx4_gemm(*a, n, *w, 1, None, n, K, out, M.MOE_DTYPE_F32, 0, env.s), "gemm")
     assert (np.abs(out.cpu().numpy() - y[:n]) <= _sum_bound(mag[:n], K)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_whose_offsets_pass_32_bits(env, dtype):
+    """Quantized from, and dequantized and multiplied into, rows 2^31 and more elements apart."""
+    M, torch = env.M, env.torch
+    rng = np.random.default_rng(13)
+    R, K, stride = 3, 300, (1 << 31) + 5
+    code, t = env.types[dtype]
+    v = rng.standard_normal((R, K)).astype(np.float32)
+    v = (v.view(np.uint32) >> 16 << 16).view(np.float32)
+    buf = torch.empty((R - 1) * stride + K + 1, dtype=t, device="cuda")
+    rows = torch.as_strided(buf, (R, K + 1), (stride, 1))
+    rows[:, :K] = torch.from_numpy(v).cuda().to(t)
+    rows[:, K] = float("nan")
+    held = env.matrix(R, K)
+    torch.cuda.synchronize()
+    env.done(M.moe_mx4_quantize(buf, code, stride, R, K, None, None, *held, env.s), "quantize")
+    padded = np.pad(v, ((0, 0), (0, -K % 32)))
+    want = X.quantize(padded)
+    c, s = X.release(held[0].cpu().numpy(), held[1].cpu().numpy(), R, K)
+    n = padded.shape[1]
+    assert ((c[:, :n] == want[0]) | ((c[:, :n] & 7) + (want[0] & 7) == 0)).all() and np.array_equal(s[:, :n // 32], want[1])
+    rows.zero_()
+    torch.cuda.synchronize()
+    env.done(M.moe_mx4_dequantize(*held, R, K, buf, code, stride, env.s), "dequantize")
+    values = X.dequantize(*want)[:, :K]
+    assert np.array_equal(rows[:, :K].float().cpu().numpy(), values.astype(np.float32)) and not rows[:, K].any()
+    w, wv = _matrix(env, rng, K, K)
+    y, mag = X.product(values, wv, [0, R], K)
+    bound = _sum_bound(mag, K) + (2.0 ** -8 * (np.abs(y) + _sum_bound(mag, K)) if dtype == "bf16" else 0.0)
+    env.done(M.moe_mx4_gemm(*held, R, *w, 1, None, K, K, buf, code, stride, env.s), "gemm")
+    assert (np.abs(rows[:, :K].float().cpu().numpy() - y) <= bound).all() and not rows[:, K].any()
