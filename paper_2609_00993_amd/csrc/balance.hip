@@ -2,9 +2,9 @@
 // (include/moepd_balance.h).
 //
 // Both directions read the logits once; what bounds them is that stream, or, for
-// small batches, the launches and dependent loads.  65,536 x 256 float32: the pieces 15.5 us
-// (4.3 TB/s), their join 7.4, the gradient 24 (5.5 TB/s); 12,001 x 512 in 37 sequences 9.5,
-// 6 and 10.5; 64 x 8 in one launch 4.  One wave takes a token at a time, its logits in
+// small batches, the launches and dependent loads.  65,536 x 256 float32: the pieces 15 us
+// (4.5 TB/s), their join 7.7, the gradient 25 (5.4 TB/s); 12,001 x 512 in 37 sequences 10.6,
+// 8.3 and 12.3; 64 x 8 in one launch 4.1.  One wave takes a token at a time, its logits in
 // registers (runs of four neighbouring experts to a lane), with wave-wide maxima and sums in
 // cross-lane moves; lanes accumulate their own experts' probabilities, so the sum
 // over tokens crosses lanes only once per piece.
@@ -15,7 +15,11 @@
 // gap in order: a piece's sums go to slot c + s, at most chunks + S - 1 slots.
 // The second kernel adds each sequence's slots in a fixed order, so the
 // results do not depend on scheduling, and its last workgroup adds the sequences'
-// losses.  Sequences of any length mix: the work is dealt by tokens.
+// losses.  The work is dealt by tokens, so long sequences share the GPU however many there
+// are; but a chunk takes its sequences one after another, and where short ones crowd beside
+// a long one, whose tokens make the chunks long, few workgroups have them all: 65,536 x 256 in 99
+// sequences of one token and one of the rest 149 us (loss alone; 100 even sequences 27),
+// 1099 and one 162 (there one wave also adds all the long one's slots; even 26).
 #include <math.h>
 
 #include <type_traits>

@@ -258,8 +258,8 @@ __device__ __forceinline__ u32x4 mx4_load(const __amdgpu_buffer_rsrc_t& rsrc, in
 // columns; one panel where there are few tiles), each slice of a panel 4 KB of
 // consecutive memory straight into registers, two slices in flight.  The waves of
 // a workgroup share a tile and deal its slices among them; their sums meet in
-// LDS and are added in wave order.  131 rows over 32 groups, 4096 x 7168: 84 us, 5.9 TB/s
-// of weights; one row, 7168 x 2048 (8 MB): 5.3 us, the launch, the tile's place, one HBM
+// LDS and are added in wave order.  131 rows over 32 groups, 4096 x 7168: 85 us, 5.8 TB/s
+// of weights; one row, 7168 x 2048 (8 MB): 4.6 us, the launch, the tile's place, one HBM
 // latency and the join.
 template <int MB, int NB>
 struct Mx4Slice4 {
