@@ -5,10 +5,12 @@
 // with one row of `a` (l % 32) and 16 of its columns, 8 q + 4 (l / 32) + (0..3).
 #include <type_traits>
 
+#include "group_tile.h"
 #include "kernels.h"
 #include "moepd_mx4.h"
 #include "mx4.h"
 #include "pipeline.h"
+#include "swiglu.h"
 #include "tiles.h"
 
 namespace moepd {
@@ -18,111 +20,6 @@ typedef float f32x16_mx4 __attribute__((ext_vector_type(16)));
 typedef float f32x4_mx4 __attribute__((ext_vector_type(4)));
 
 namespace {
-
-struct Mx4Tile {  // wave-uniform
-  int group;
-  int m0, m_end;  // rows
-  int nt;         // column tile
-};
-
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ long long uniform(long long v) {
-  return (long long)(((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v));
-}
-
-// Inclusive sum over the wave's lanes (register moves across lanes; see common.h).
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ int dpp_plus(int v) {
-  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xF, false);
-}
-__device__ __forceinline__ int wave_scan(int v) {
-  v = dpp_plus<0x111, 0xF>(v);  // row_shr:1
-  v = dpp_plus<0x112, 0xF>(v);  // row_shr:2
-  v = dpp_plus<0x114, 0xF>(v);  // row_shr:4
-  v = dpp_plus<0x118, 0xF>(v);  // row_shr:8
-  v = dpp_plus<0x142, 0xA>(v);  // row_bcast:15
-  return dpp_plus<0x143, 0xC>(v);  // row_bcast:31
-}
-
-// The tile of workgroup b, if any, found by each wave from the offsets: lane i
-// holds group i's rows, and a scan of the groups' counts of row tiles (of at most bm
-// rows) places the tile; with more than 64 groups, 64 at a time.
-//
-// STRIPED (streaming tiles): groups in order, within a group of mt row tiles column
-// tile 8 q + b % 8 for each q, with all its row tiles in a row: workgroup b runs on
-// XCD b % 8, so the row tiles that read one weight panel share an L2, and every XCD
-// streams an eighth of every group's weights.
-//
-// Otherwise (ring tiles): a group's rows are shared evenly among its row tiles; its
-// tiles run over blocks of four column tiles, in each row tile by row tile; and runs of
-// consecutive tiles are dealt to the XCDs in turn, so that an XCD's L2 serves each row
-// block to four workgroups and each weight panel to as many as the run has row
-// tiles.  The last runs, when they do not go round, are dealt tile by tile.  Runs of 64 tiles
-// (16 row x 4 column tiles: what an XCD's CUs hold at a time) for groups of many rows,
-// else 32, which leave less to the last round: 96,889 skewed rows (7168 x 2048)
-// 1030 us with 64, 1096 with 32; 32,768 rows 391 / 430; 8192 rows, 256 to a group, 77 / 73.
-template <bool STRIPED>
-__device__ __forceinline__ bool mx4_tile(const Mx4Args& g, int b, int bm, Mx4Tile& t) {
-  const int lane = lane_id();
-  int l = 0, h = 0, mt = 0, incl = 0;  // of group g0 + lane
-  auto count = [&](int g0) {
-    l = h = 0;
-    const int e = g0 + lane;
-    if (!g.offsets) {
-      h = lane == 0 ? g.rows : 0;
-    } else if (e < g.groups) {
-      const int a = g.offsets[e], z = g.offsets[e + 1];
-      l = min(max(a, 0), g.rows);
-      h = max(l, min(z, g.rows));
-    }
-    mt = (int)((unsigned)(h - l + bm - 1) / (unsigned)bm);
-    incl = wave_scan(mt);
-    return __builtin_amdgcn_readlane(incl, 63);
-  };
-  int m_here = count(0);
-  int L = b;
-  if constexpr (!STRIPED) {
-    int m_total = m_here;
-    if (g.groups > kWave) {
-      for (int g0 = kWave; g0 < g.groups; g0 += kWave) m_total += count(g0);
-      m_here = count(0);
-    }
-    const int total = m_total * g.n_tiles;
-    const int x = b & 7, slot = b >> 3, round = slot / g.run, base = round * 8 * g.run, j = slot - round * g.run;
-    L = base + 8 * g.run <= total ? base + x * g.run + j : base + 8 * j + x;
-    if (L >= total) return false;
-  }
-  int want = (int)((unsigned)L / (unsigned)g.n_tiles);  // row tiles before this one
-  int at = L - want * g.n_tiles, g0 = 0;
-  while (want >= m_here) {
-    want -= m_here;
-    g0 += kWave;
-    if (g0 >= g.groups) return false;
-    m_here = count(g0);
-  }
-  const uint64_t past = __ballot(incl > want);
-  if (!past) return false;
-  const int src = __builtin_ctzll(past);
-  const int mt_e = __builtin_amdgcn_readlane(mt, src);
-  const int lo = __builtin_amdgcn_readlane(l, src), hi = __builtin_amdgcn_readlane(h, src);
-  at += (want - (__builtin_amdgcn_readlane(incl, src) - mt_e)) * g.n_tiles;  // within the group
-  t.group = uniform(g0 + src);
-  if constexpr (STRIPED) {
-    const int j = at >> 3, q = j / mt_e;
-    t.nt = uniform(8 * q + (at & 7));
-    t.m0 = uniform(lo + (j - q * mt_e) * bm);
-    t.m_end = uniform(min(t.m0 + bm, hi));
-  } else {
-    const int q = at / (4 * mt_e), r = at - q * 4 * mt_e;
-    const int width = min(4, g.n_tiles - 4 * q);
-    const int mi = r / width;
-    t.nt = uniform(4 * q + r - mi * width);
-    const int per = (hi - lo + mt_e - 1) / mt_e;
-    t.m0 = uniform(lo + mi * per);
-    t.m_end = uniform(min(t.m0 + per, hi));
-  }
-  return true;
-}
 
 __device__ __forceinline__ v8i32_mx4 widen(const u32x4& a) {
   return v8i32_mx4{(int32_t)a[0], (int32_t)a[1], (int32_t)a[2], (int32_t)a[3], 0, 0, 0, 0};
@@ -134,33 +31,6 @@ template <int S>
 __device__ __forceinline__ f32x16_mx4 mx4_mfma(const u32x4& w, const u32x4& a, const f32x16_mx4& acc, uint32_t sw,
                                                uint32_t sa) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(w), widen(a), acc, 4, 4, S, (int)sw, S, (int)sa);
-}
-
-// silu(g) * u.  With q = e^-|g|, silu is g / (1 + q), times q where g is negative: q never
-// overflows, and 1 + q is between 1 and 2.  q as 2^(t + lo): the product's rounding error and
-// log2 e's own, lo, would otherwise cost |g| ulp; with it, and the hardware's 2^x and
-// reciprocal (1 ulp each), the result is within a few ulp.  Far below zero q and g q pass
-// below the normal numbers (which the hardware's 2^x flushes), at -87 and -92, while u may
-// bring the result back: there q carries a factor of 2^64 that 1 + q leaves out and u gives
-// back, good down to gates of -131.  Past 256 q is 0 in any case.
-__device__ __forceinline__ float mx4_silu_mul(float g, float u) {
-#pragma clang fp contract(off)  // t + 64 must start from the rounded t, whose error lo holds
-  constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
-  const float a = fminf(__builtin_fabsf(g), 256.f);
-  const float t = -a * kLog2e;
-  const float lo = __builtin_fmaf(-a, kLog2eLow, __builtin_fmaf(-a, kLog2e, -t));
-  const bool deep = g < -44.f;
-  const float k = deep ? 0x1p-64f : 1.f;
-  const float e = __builtin_amdgcn_exp2f(t + (deep ? 64.f : 0.f));
-  const float q = __builtin_fmaf(e, lo * kLn2, e);
-  return (g < 0.f ? g * q : g) * __builtin_amdgcn_rcpf(__builtin_fmaf(q, k, 1.f)) * (u * k);
-}
-
-// Two values to bf16, nearest even, packed.
-__device__ __forceinline__ uint32_t mx4_bf16_pair(float a, float b) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
 // Store one 32 x 32 block: lane (r, h) holds v[4 q + t] = column col0 + 8 q + 4 h + t of `row`.
@@ -205,7 +75,7 @@ __device__ __forceinline__ void mx4_store(const Mx4Args& g, const float (&v)[16]
         } else {
           typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
           *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(g.c) + at + 8 * q) =
-              u32x2{mx4_bf16_pair(v[4 * q], v[4 * q + 1]), mx4_bf16_pair(v[4 * q + 2], v[4 * q + 3])};
+              u32x2{bf16_pair(v[4 * q], v[4 * q + 1]), bf16_pair(v[4 * q + 2], v[4 * q + 3])};
         }
       } else {
 #pragma unroll
@@ -268,7 +138,7 @@ struct Mx4Slice4 {
 };
 
 template <int MB, int NB, bool GATED, int OUT>
-__device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile& t, float* lds) {
+__device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const GroupTile& t, float* lds) {
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int KT = g.slices;
@@ -382,7 +252,7 @@ __device__ __forceinline__ void mx4_stream_tile(const Mx4Args& g, const Mx4Tile&
     float v[16];
     if constexpr (GATED) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = mx4_silu_mul(acc[m][0][i], acc[m][NB - 1][i]);
+      for (int i = 0; i < 16; ++i) v[i] = swiglu_of(acc[m][0][i], acc[m][NB - 1][i]);
       mx4_store<OUT>(g, v, row, live, n0, h);
     } else {
 #pragma unroll
@@ -401,8 +271,8 @@ template <int MAXB, int NB, bool GATED, int OUT>
 __global__ __launch_bounds__(64 * kStreamWaves, MAXB == 2 ? 2 : NB == 2 ? 3 : 4) void mx4_stream_kernel(
     Mx4Args g) {
   extern __shared__ __align__(16) float lds[];
-  Mx4Tile t;
-  if (!mx4_tile<true>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), 32 * MAXB, t)) return;
+  GroupTile t;
+  if (!group_tile<true>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), 32 * MAXB, t)) return;
   if (t.nt * (GATED ? 32 : 32 * NB) >= (OUT == kMx4Fp4 ? (g.n + kMx4Slice - 1) / kMx4Slice * kMx4Slice : g.n)) return;
   if constexpr (MAXB == 1) {
     mx4_stream_tile<1, NB, GATED, OUT>(g, t, lds);
@@ -432,7 +302,7 @@ struct Mx4Patch {
       if constexpr (OUT == kMx4F32)
         *reinterpret_cast<f32x4_mx4*>(p) = f32x4_mx4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
       else
-        *reinterpret_cast<u32x2*>(p) = u32x2{mx4_bf16_pair(v[4 * q], v[4 * q + 1]), mx4_bf16_pair(v[4 * q + 2], v[4 * q + 3])};
+        *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pair(v[4 * q], v[4 * q + 1]), bf16_pair(v[4 * q + 2], v[4 * q + 3])};
     }
   }
 
@@ -489,7 +359,7 @@ struct Mx4Patch {
 // no memory, and every slice has the same instructions, so the counted waits are exact
 // throughout.
 template <int MB, int SA, bool GATED, int OUT>
-__device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t, u32x4* lds) {
+__device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const GroupTile& t, u32x4* lds) {
   constexpr int kSlot = MB * 256;  // 16-byte units
   static_assert(SA >= 3, "the wait below counts whole slices between a slot's request and its use");
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
@@ -651,7 +521,7 @@ __device__ __forceinline__ void mx4_ring_tile(const Mx4Args& g, const Mx4Tile& t
     float v[16];
     if constexpr (GATED) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = mx4_silu_mul(acc[m][0][i], acc[m][1][i]);
+      for (int i = 0; i < 16; ++i) v[i] = swiglu_of(acc[m][0][i], acc[m][1][i]);
       if constexpr (OUT == kMx4Fp4) mx4_store<OUT>(g, v, m0 + 32 * m + r, 32 * m + r < m_rows, n0, h);
       else Mx4Patch<OUT, COLS>::put(part, v, 0, r, h);
     } else {
@@ -674,8 +544,8 @@ template <bool GATED, int OUT>
 __global__ __launch_bounds__(256, 2) void mx4_ring_kernel(Mx4Args g) {
   constexpr int ring = kRingSlots * kRingBlocks * 256, parts = 4 * Mx4Patch<OUT, GATED ? 32 : 64>::bytes / 16;
   __shared__ u32x4 lds[ring > parts ? ring : parts];
-  Mx4Tile t;
-  if (!mx4_tile<false>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), 32 * kRingBlocks, t)) return;
+  GroupTile t;
+  if (!group_tile<false>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), 32 * kRingBlocks, t)) return;
   const int blocks = (t.m_end - t.m0 + 31) / 32;
   if (blocks <= 0) return;  // fewer rows than tiles: an even share of none
   weave_run<1, kRingBlocks + 1>([&](auto mb) {

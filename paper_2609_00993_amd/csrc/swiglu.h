@@ -1,0 +1,53 @@
+// SwiGLU in float32 and conversions of its results, shared by the products that end in it.
+#pragma once
+
+#include "common.h"
+
+namespace moepd {
+
+// silu(g) * u.  With q = e^-|g|, silu is g / (1 + q), times q where g is negative: q never
+// overflows, and 1 + q is between 1 and 2.  q as 2^(t + lo): the product's rounding error and
+// log2 e's own, lo, would otherwise cost |g| ulp; with it, and the hardware's 2^x and
+// reciprocal (1 ulp each), the result is within a few ulp.  Far below zero q and g q pass
+// below the normal numbers (which the hardware's 2^x flushes), at -87 and -92, while u may
+// bring the result back: there q carries a factor of 2^64 that 1 + q leaves out and u gives
+// back, good down to gates of -131.  Past 256 q is 0 in any case.
+__device__ __forceinline__ float swiglu_of(float g, float u) {
+#pragma clang fp contract(off)  // t + 64 must start from the rounded t, whose error lo holds
+  constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
+  const float a = fminf(__builtin_fabsf(g), 256.f);
+  const float t = -a * kLog2e;
+  const float lo = __builtin_fmaf(-a, kLog2eLow, __builtin_fmaf(-a, kLog2e, -t));
+  const bool deep = g < -44.f;
+  const float k = deep ? 0x1p-64f : 1.f;
+  const float e = __builtin_amdgcn_exp2f(t + (deep ? 64.f : 0.f));
+  const float q = __builtin_fmaf(e, lo * kLn2, e);
+  return (g < 0.f ? g * q : g) * __builtin_amdgcn_rcpf(__builtin_fmaf(q, k, 1.f)) * (u * k);
+}
+
+// From dh to the gradients in gate and up: dg = dh u s (1 + g (1 - s)), du = dh g s, with s =
+// 1 / (1 + e^-g) from q = e^-|g|, which never overflows.  g q is 0 from where q is, infinite
+// gates included.
+__device__ __forceinline__ void swiglu_grad(float g, float u, float dh, float& dg, float& du) {
+#pragma clang fp contract(off)
+  constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
+  const float a = __builtin_fabsf(g) > 256.f ? 256.f : __builtin_fabsf(g);  // NaN stays
+  const float t = -a * kLog2e;
+  const float lo = __builtin_fmaf(-a, kLog2eLow, __builtin_fmaf(-a, kLog2e, -t));  // see swiglu_of
+  const float e = __builtin_amdgcn_exp2f(t);
+  const float q = __builtin_fmaf(e, lo * kLn2, e);
+  const float near = __builtin_amdgcn_rcpf(1.f + q), far = q * near;  // s and 1 - s where g >= 0
+  const float s = g < 0.f ? far : near;
+  const float rest = a * (g < 0.f ? -near : far);  // g (1 - s)
+  dg = dh * u * s * (1.f + rest);
+  du = dh * ((g < 0.f ? -a : g) * s);
+}
+
+// Two values to bf16, nearest even, packed.
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+}  // namespace moepd
