@@ -1,0 +1,367 @@
+// The gated feed-forward block and its backward pass (include/moepd_ffn.h): tiles, launches and
+// the C entry points.  The tile itself is in ffn_ring.h (bf16) and ffn_block_f32.h.
+#include <type_traits>
+
+#include "common.h"
+#include "ffn_ring.h"
+#include "ffn_block_f32.h"
+#include "kernels.h"
+#include "moepd_ffn.h"
+#include "tiles.h"
+
+namespace moepd {
+namespace {
+
+// ------------------------------------------------------------------ rows times a group's weights
+
+__device__ __forceinline__ bool ffn_row_tile(const FfnArgs& g, int bm, int bn, FfnTile& t) {
+  GroupTile w;
+  if (!group_tile<false>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), bm, w)) return false;
+  t.group = w.group;
+  t.m0 = w.m0;
+  t.rows = w.m_end - w.m0;
+  t.n0 = w.nt * bn;
+  t.k0 = t.k_count = 0;
+  return true;
+}
+
+// Tiles of up to 160 rows, cut to the 32-row blocks that they hold; four waves side by side
+// along the columns.
+constexpr int kFfnMidRows = 160;
+template <int KIND, bool F32>
+__global__ __launch_bounds__(256) void ffn_block_mid(FfnArgs g) {
+  __shared__ u32x4 lds[ffn_chunks(kFfnMidRows, 256, 3, 3)];
+  FfnTile t;
+  if (!ffn_row_tile(g, kFfnMidRows, KIND == kFfnGateUp ? 128 : 256, t)) return;
+  const int blocks = (t.rows + 31) / 32;
+  if (blocks <= 1) ffn_tile<KIND, F32, 32, 256, 1, 4, 3, 3>(g, t, g.c, lds);
+  else if (blocks == 2) ffn_tile<KIND, F32, 64, 256, 1, 4, 3, 3>(g, t, g.c, lds);
+  else if (blocks == 3) ffn_tile<KIND, F32, 96, 256, 1, 4, 3, 3>(g, t, g.c, lds);
+  else if (blocks == 4) ffn_tile<KIND, F32, 128, 256, 1, 4, 3, 3>(g, t, g.c, lds);
+  else ffn_tile<KIND, F32, 160, 256, 1, 4, 3, 3>(g, t, g.c, lds);
+}
+
+// ------------------------------------------------------------------ gradients of the weights
+
+// Workgroup b's tile: parts of the rows outermost, then groups; within a group blocks of four
+// column tiles, row tile by row tile; runs of consecutive tiles dealt to the XCDs in turn.
+__device__ __forceinline__ bool ffn_weight_tile(const FfnArgs& g, int bm, int bn, FfnTile& t, int& split) {
+  const int b = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+  const int per = g.m_tiles * g.n_tiles, total = per * g.groups * g.splits;
+  const int x = b & 7, slot = b >> 3, round = slot / g.run, base = round * 8 * g.run, j = slot - round * g.run;
+  const int L = uniform(base + 8 * g.run <= total ? base + x * g.run + j : base + 8 * j + x);
+  if (L >= total) return false;
+  const int sg = L / per, at = L - sg * per;
+  split = sg / g.groups;
+  t.group = sg - split * g.groups;
+  const int q = at / (4 * g.m_tiles), r = at - q * 4 * g.m_tiles;
+  const int width = min(4, g.n_tiles - 4 * q);
+  const int mi = r / width;
+  t.m0 = mi * bm;
+  t.rows = min(bm, g.m - t.m0);
+  t.n0 = (4 * q + r - mi * width) * bn;
+  int lo = 0, hi = g.rows;
+  if (g.offsets) {
+    lo = uniform(min(max(g.offsets[t.group], 0), g.rows));
+    hi = uniform(max(lo, min(g.offsets[t.group + 1], g.rows)));
+  }
+  const int part = (hi - lo + g.splits - 1) / g.splits;
+  const int each = (part + kFfnSlice - 1) / kFfnSlice * kFfnSlice;
+  t.k0 = min((long long)hi, lo + (long long)split * each);
+  t.k_count = min(each, hi - t.k0);
+  return true;
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256, 2) void ffn_block_weights(FfnArgs g) {
+  __shared__ u32x4 lds[ffn_chunks(128, 128, 2, 2)];
+  FfnTile t;
+  int split;
+  if (!ffn_weight_tile(g, 128, 128, t, split)) return;
+  uint8_t* c = g.c + ((long long)split * g.groups + t.group) * g.m * g.ldc;
+  ffn_tile<kFfnWeightGrad, F32, 128, 128, 2, 2, 2, 2>(g, t, c, lds);
+}
+
+// The parts' sums, in order, to the result.
+template <bool F32>
+__global__ __launch_bounds__(256) void ffn_block_join(const float* parts, long long values, int splits, int accumulate,
+                                                      uint8_t* out) {
+  const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (at >= values) return;
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  for (int s = 0; s < splits; ++s) {
+    const f32x4_ffn* p = reinterpret_cast<const f32x4_ffn*>(parts + s * values + at);
+    const f32x4_ffn lo = p[0], hi = p[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] += lo[i];
+      v[4 + i] += hi[i];
+    }
+  }
+  uint8_t* p = out + at * (F32 ? 4 : 2);
+  if (accumulate) {
+    float old[8];
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) old[i] = reinterpret_cast<const float*>(p)[i];
+    } else {
+      ffn_unpack8(load16(p), old);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += old[i];
+  }
+  if constexpr (F32) {
+    store16(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+    store16(p + 16, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+  } else {
+    store16(p, ffn_bf16x8(v));
+  }
+}
+
+// ------------------------------------------------------------------ host side
+
+constexpr long long kMostBlocks = (1LL << 31) - (1 << 16);
+
+bool launched() { return hipGetLastError() == hipSuccess; }
+
+int launch_rows(FfnArgs g, int kind, bool out_f32, bool f32, hipStream_t s) {
+  if (f32) {
+    g.n_tiles = (g.n + kFfnF32Cols - 1) / kFfnF32Cols;
+    g.run = 32;
+    const long long tiles = (g.rows / kFfnF32Rows + (long long)g.groups) * g.n_tiles;
+    if (tiles > kMostBlocks) return MOE_ERR_INVALID_ARG;
+    const dim3 grid = grid_of((tiles + 7) / 8 * 8, 256);
+    switch (kind) {
+      case kFfnGateUp: ffn_block_f32<kFfnGateUp><<<grid, 256, 0, s>>>(g); break;
+      case kFfnDown: ffn_block_f32<kFfnDown><<<grid, 256, 0, s>>>(g); break;
+      case kFfnDownGrad: ffn_block_f32<kFfnDownGrad><<<grid, 256, 0, s>>>(g); break;
+      default: ffn_block_f32<kFfnGateUpGrad><<<grid, 256, 0, s>>>(g);
+    }
+    return launched() ? MOE_OK : MOE_ERR_HIP;
+  }
+  const int bn = kind == kFfnGateUp ? 128 : 256;
+  g.n_tiles = (g.n + bn - 1) / bn;
+  g.run = 32;
+  const long long tiles = (g.rows / kFfnMidRows + (long long)g.groups) * g.n_tiles;
+  if (tiles > kMostBlocks) return MOE_ERR_INVALID_ARG;
+  const dim3 grid = grid_of((tiles + 7) / 8 * 8, 256);
+  switch (kind) {
+    case kFfnGateUp: ffn_block_mid<kFfnGateUp, false><<<grid, 256, 0, s>>>(g); break;
+    case kFfnDown:
+      if (out_f32) ffn_block_mid<kFfnDown, true><<<grid, 256, 0, s>>>(g);
+      else ffn_block_mid<kFfnDown, false><<<grid, 256, 0, s>>>(g);
+      break;
+    case kFfnDownGrad: ffn_block_mid<kFfnDownGrad, false><<<grid, 256, 0, s>>>(g); break;
+    default:
+      if (out_f32) ffn_block_mid<kFfnGateUpGrad, true><<<grid, 256, 0, s>>>(g);
+      else ffn_block_mid<kFfnGateUpGrad, false><<<grid, 256, 0, s>>>(g);
+  }
+  return launched() ? MOE_OK : MOE_ERR_HIP;
+}
+
+constexpr int kMostWidth = 32768;
+constexpr long long kMostStride = 1 << 20;
+
+bool shape_ok(int64_t rows, int32_t groups, const int32_t* offsets, int32_t H, int32_t I, int32_t dtype, hipStream_t s) {
+  if (!s || rows < 0 || rows > (1LL << 31) - 512) return false;
+  if (groups < 1 || groups > 1024 || (!offsets && groups != 1) || (uintptr_t)offsets % 4) return false;
+  if (H < 8 || H > kMostWidth || H % 8 || I < 8 || I > kMostWidth || I % 8 || (long long)H * I > (1 << 28)) return false;
+  return dtype == MOE_DTYPE_F32 || dtype == MOE_DTYPE_BF16;
+}
+
+bool stride_ok(int64_t* stride, int width) {
+  if (*stride == 0) *stride = width;
+  return *stride >= width && *stride <= kMostStride && *stride % 8 == 0;
+}
+
+bool out_ok(int32_t out, int32_t dtype) { return out == MOE_DTYPE_F32 || (out == MOE_DTYPE_BF16 && dtype == MOE_DTYPE_BF16); }
+
+template <class... P>
+bool aligned16(const P*... p) {
+  return ((0 | ... | (uintptr_t)p) % 16) == 0;
+}
+
+int size_of(int32_t dtype) { return dtype == MOE_DTYPE_F32 ? 4 : 2; }
+
+// Parts of the rows for the weights' gradient: enough tiles to fill the GPU twice, and at
+// least four slices to a part.  128 x 128 tiles of 64 KB: 512 of them are 2^25 bytes.
+int weight_splits(long long rows, int groups, long long tiles) {
+  const long long slices = rows / groups / kFfnSlice;
+  long long s = (512 + tiles - 1) / tiles;
+  s = s < slices / 4 ? s : slices / 4;
+  return tiles >= 384 || s < 2 ? 1 : (int)s;
+}
+long long weight_tiles(int groups, int m, int n) { return (long long)groups * ((m + 127) / 128) * ((n + 127) / 128); }
+long long weight_bytes(long long rows, int groups, int m, int n) {
+  const int s = weight_splits(rows, groups, weight_tiles(groups, m, n));
+  return s > 1 ? 4LL * s * groups * m * n : 0;
+}
+bool weight_shape_ok(int64_t rows, int32_t groups, int32_t m, int32_t n) {
+  return rows >= 0 && rows <= (1LL << 31) - 512 && groups >= 1 && groups <= 1024 && m >= 8 && n >= 8 && m % 8 == 0 &&
+         n % 8 == 0 && m <= 2 * kMostWidth && n <= 2 * kMostWidth && (long long)m * n <= (1 << 29);
+}
+
+}  // namespace
+}  // namespace moepd
+
+using namespace moepd;
+
+extern "C" {
+
+int moe_ffn_gate_up(const void* x, int64_t x_stride, int64_t rows, const void* w_gate_up, int32_t groups,
+                    const int32_t* offsets, int32_t hidden, int32_t inter, int32_t dtype, void* gate_up, void* h,
+                    hipStream_t stream) {
+  if (!shape_ok(rows, groups, offsets, hidden, inter, dtype, stream) || !stride_ok(&x_stride, hidden))
+    return MOE_ERR_INVALID_ARG;
+  if (!aligned16(x, w_gate_up, gate_up, h)) return MOE_ERR_INVALID_ARG;
+  if (rows == 0) return MOE_OK;
+  if (!x || !w_gate_up || !h) return MOE_ERR_INVALID_ARG;
+  const int sz = size_of(dtype);
+  FfnArgs g{};
+  g.a = (const uint8_t*)x;
+  g.b = (const uint8_t*)w_gate_up;
+  g.c = (uint8_t*)gate_up;
+  g.h = (uint8_t*)h;
+  g.lda = x_stride * sz;
+  g.ldb = (long long)hidden * sz;
+  g.b_group = 2LL * inter * hidden * sz;
+  g.offsets = offsets;
+  g.rows = (int)rows;
+  g.groups = groups;
+  g.n = inter;
+  g.k = hidden;
+  return launch_rows(g, kFfnGateUp, false, dtype == MOE_DTYPE_F32, stream);
+}
+
+int moe_ffn_down(const void* h, int64_t rows, const void* w_down, int32_t groups, const int32_t* offsets, int32_t hidden,
+                 int32_t inter, int32_t dtype, void* y, int32_t y_dtype, int64_t y_stride, hipStream_t stream) {
+  if (!shape_ok(rows, groups, offsets, hidden, inter, dtype, stream) || !stride_ok(&y_stride, hidden) ||
+      !out_ok(y_dtype, dtype) || !aligned16(h, w_down, y))
+    return MOE_ERR_INVALID_ARG;
+  if (rows == 0) return MOE_OK;
+  if (!h || !w_down || !y) return MOE_ERR_INVALID_ARG;
+  const int sz = size_of(dtype);
+  FfnArgs g{};
+  g.a = (const uint8_t*)h;
+  g.b = (const uint8_t*)w_down;
+  g.c = (uint8_t*)y;
+  g.lda = (long long)inter * sz;
+  g.ldb = (long long)inter * sz;
+  g.ldc = y_stride * size_of(y_dtype);
+  g.b_group = (long long)inter * hidden * sz;
+  g.offsets = offsets;
+  g.rows = (int)rows;
+  g.groups = groups;
+  g.n = hidden;
+  g.k = inter;
+  return launch_rows(g, kFfnDown, y_dtype == MOE_DTYPE_F32, dtype == MOE_DTYPE_F32, stream);
+}
+
+int moe_ffn_down_backward(const void* dy, int64_t dy_stride, int64_t rows, const void* w_down, const void* gate_up,
+                          int32_t groups, const int32_t* offsets, int32_t hidden, int32_t inter, int32_t dtype,
+                          void* dgate_up, void* h, hipStream_t stream) {
+  if (!shape_ok(rows, groups, offsets, hidden, inter, dtype, stream) || !stride_ok(&dy_stride, hidden) ||
+      !aligned16(dy, w_down, gate_up, dgate_up, h))
+    return MOE_ERR_INVALID_ARG;
+  if (rows == 0) return MOE_OK;
+  if (!dy || !w_down || !gate_up || !dgate_up) return MOE_ERR_INVALID_ARG;
+  const int sz = size_of(dtype);
+  FfnArgs g{};
+  g.a = (const uint8_t*)dy;
+  g.b = (const uint8_t*)w_down;
+  g.c = (uint8_t*)dgate_up;
+  g.h = (uint8_t*)h;
+  g.gu = (const uint8_t*)gate_up;
+  g.lda = dy_stride * sz;
+  g.ldb = (long long)inter * sz;
+  g.b_group = (long long)inter * hidden * sz;
+  g.offsets = offsets;
+  g.rows = (int)rows;
+  g.groups = groups;
+  g.n = inter;
+  g.k = hidden;
+  return launch_rows(g, kFfnDownGrad, false, dtype == MOE_DTYPE_F32, stream);
+}
+
+int moe_ffn_gate_up_backward(const void* dgate_up, int64_t rows, const void* w_gate_up, int32_t groups,
+                             const int32_t* offsets, int32_t hidden, int32_t inter, int32_t dtype, void* dx,
+                             int32_t dx_dtype, int64_t dx_stride, hipStream_t stream) {
+  if (!shape_ok(rows, groups, offsets, hidden, inter, dtype, stream) || !stride_ok(&dx_stride, hidden) ||
+      !out_ok(dx_dtype, dtype) || !aligned16(dgate_up, w_gate_up, dx))
+    return MOE_ERR_INVALID_ARG;
+  if (rows == 0) return MOE_OK;
+  if (!dgate_up || !w_gate_up || !dx) return MOE_ERR_INVALID_ARG;
+  const int sz = size_of(dtype);
+  FfnArgs g{};
+  g.a = (const uint8_t*)dgate_up;
+  g.b = (const uint8_t*)w_gate_up;
+  g.c = (uint8_t*)dx;
+  g.lda = 2LL * inter * sz;
+  g.ldb = (long long)hidden * sz;
+  g.ldc = dx_stride * size_of(dx_dtype);
+  g.b_group = 2LL * inter * hidden * sz;
+  g.offsets = offsets;
+  g.rows = (int)rows;
+  g.groups = groups;
+  g.n = hidden;
+  g.k = 2 * inter;
+  return launch_rows(g, kFfnGateUpGrad, dx_dtype == MOE_DTYPE_F32, dtype == MOE_DTYPE_F32, stream);
+}
+
+int moe_ffn_weight_workspace(int64_t rows, int32_t groups, int32_t m, int32_t n, int64_t* bytes) {
+  if (!bytes || !weight_shape_ok(rows, groups, m, n)) return MOE_ERR_INVALID_ARG;
+  *bytes = weight_bytes(rows, groups, m, n);
+  return MOE_OK;
+}
+
+int moe_ffn_weight_grad(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t rows, int32_t groups,
+                        const int32_t* offsets, int32_t m, int32_t n, int32_t dtype, void* dw, int32_t dw_dtype,
+                        int32_t accumulate, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+  if (!stream || !weight_shape_ok(rows, groups, m, n) || (!offsets && groups != 1) || (uintptr_t)offsets % 4 ||
+      !stride_ok(&a_stride, m) || !stride_ok(&b_stride, n) || (dtype != MOE_DTYPE_F32 && dtype != MOE_DTYPE_BF16) ||
+      !out_ok(dw_dtype, dtype) || !aligned16(a, b, dw) || !dw || (uintptr_t)workspace % 256)
+    return MOE_ERR_INVALID_ARG;
+  if (rows > 0 && (!a || !b)) return MOE_ERR_INVALID_ARG;
+  const long long need = weight_bytes(rows, groups, m, n);
+  if (need > 0 && !workspace) return MOE_ERR_INVALID_ARG;
+  if (need > workspace_bytes) return MOE_ERR_CAPACITY;
+  const int sz = size_of(dtype);
+  const bool f32 = dw_dtype == MOE_DTYPE_F32;
+  FfnArgs g{};
+  g.a = (const uint8_t*)a;
+  g.b = (const uint8_t*)b;
+  g.lda = a_stride * sz;
+  g.ldb = b_stride * sz;
+  g.offsets = offsets;
+  g.rows = (int)rows;
+  g.groups = groups;
+  g.m = m;
+  g.n = n;
+  g.run = 32;
+  g.splits = need > 0 ? weight_splits(rows, groups, weight_tiles(groups, m, n)) : 1;
+  g.c = g.splits > 1 ? (uint8_t*)workspace : (uint8_t*)dw;
+  g.accumulate = g.splits > 1 ? 0 : accumulate != 0;
+  g.ldc = (long long)n * (g.splits > 1 ? 4 : size_of(dw_dtype));
+  const int edge = dtype == MOE_DTYPE_F32 ? kFfnF32Rows : 128;
+  g.m_tiles = (m + edge - 1) / edge;
+  g.n_tiles = (n + edge - 1) / edge;
+  const long long tiles = (long long)g.m_tiles * g.n_tiles * groups * g.splits;
+  if (tiles > kMostBlocks) return MOE_ERR_INVALID_ARG;
+  const dim3 grid = grid_of((tiles + 7) / 8 * 8, 256);
+  if (dtype == MOE_DTYPE_F32) ffn_block_f32_weights<<<grid, 256, 0, stream>>>(g);
+  else if (f32 || g.splits > 1) ffn_block_weights<true><<<grid, 256, 0, stream>>>(g);
+  else ffn_block_weights<false><<<grid, 256, 0, stream>>>(g);
+  if (!launched()) return MOE_ERR_HIP;
+  if (g.splits > 1) {
+    const long long values = (long long)groups * m * n;
+    const dim3 blocks((unsigned)((values / 8 + 255) / 256));
+    if (f32) ffn_block_join<true><<<blocks, 256, 0, stream>>>((const float*)workspace, values, g.splits, accumulate != 0, (uint8_t*)dw);
+    else ffn_block_join<false><<<blocks, 256, 0, stream>>>((const float*)workspace, values, g.splits, accumulate != 0, (uint8_t*)dw);
+    if (!launched()) return MOE_ERR_HIP;
+  }
+  return MOE_OK;
+}
+
+}  // extern "C"

@@ -1,5 +1,6 @@
 """Thin ctypes binding of libmoepd (the C ABI declared in include/moepd.h,
-include/moepd_mx4.h, include/moepd_balance.h and include/moepd_turnstile.h).
+include/moepd_mx4.h, include/moepd_balance.h, include/moepd_ffn.h, include/moepd_rows.h,
+include/moepd_adamw.h and include/moepd_turnstile.h).
 
 Argument marshalling only: every step of the layer runs in the HIP library.
 Device buffers may be passed as integers (device addresses) or as objects
@@ -17,7 +18,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_uint32, c_void_p
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libmoepd.so")
@@ -125,6 +126,22 @@ class moe_p_epoch_stats_t(ctypes.Structure):
     ]
 
 
+class moe_adamw_tensor_t(ctypes.Structure):
+    _fields_ = [
+        ("param", c_void_p),
+        ("master", c_void_p),
+        ("grad", c_void_p),
+        ("m", c_void_p),
+        ("v", c_void_p),
+        ("m_scales", c_void_p),
+        ("v_scales", c_void_p),
+        ("n", c_int64),
+        ("weight_decay", c_double),
+        ("param_dtype", c_int32),
+        ("grad_dtype", c_int32),
+    ]
+
+
 # Every symbol the headers declare, with its ctypes signature.
 _SIGNATURES = {
     "moe_ctx_create": (c_int, [POINTER(moe_config_t), POINTER(moe_weights_t), POINTER(c_void_p)]),
@@ -160,6 +177,30 @@ _SIGNATURES = {
     "moe_balance_loss_backward": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_int32, c_int32, c_int32,
                                           c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int32,
                                           c_void_p]),
+    "moe_ffn_gate_up": (c_int, [c_void_p, c_int64, c_int64, c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32, c_void_p,
+                                c_void_p, c_void_p]),
+    "moe_ffn_down": (c_int, [c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int32,
+                             c_int64, c_void_p]),
+    "moe_ffn_down_backward": (c_int, [c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_int32, c_void_p, c_int32, c_int32,
+                                      c_int32, c_void_p, c_void_p, c_void_p]),
+    "moe_ffn_gate_up_backward": (c_int, [c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32, c_void_p,
+                                         c_int32, c_int64, c_void_p]),
+    "moe_ffn_weight_workspace": (c_int, [c_int64, c_int32, c_int32, c_int32, POINTER(c_int64)]),
+    "moe_ffn_weight_grad": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int32, c_void_p, c_int32, c_int32,
+                                    c_int32, c_void_p, c_int32, c_int32, c_void_p, c_int64, c_void_p]),
+    "moe_rows_gather": (c_int, [c_void_p, c_int32, c_int64, c_int32, c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_int64,
+                                c_void_p]),
+    "moe_rows_combine": (c_int, [c_void_p, c_int32, c_int64, c_int64, c_void_p, c_void_p, c_int32, c_int32, c_int32,
+                                 c_void_p, c_int32, c_int64, c_void_p]),
+    "moe_rows_combine_backward": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_int64, c_void_p,
+                                          c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int32, c_int64, c_void_p,
+                                          c_void_p]),
+    "moe_gate_backward": (c_int, [c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int32, c_int64,
+                                  c_int32, c_void_p]),
+    "moe_adamw_create": (c_int, [POINTER(moe_adamw_tensor_t), c_int32, c_int32, POINTER(c_void_p)]),
+    "moe_adamw_step": (c_int, [c_void_p, c_double, c_double, c_double, c_void_p, c_void_p, c_void_p, c_uint32, c_void_p]),
+    "moe_adamw_read": (c_int, [c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p]),
+    "moe_adamw_destroy": (c_int, [c_void_p]),
     "moe_turnstile_create": (c_int, [c_int32, c_int32, POINTER(c_void_p)]),
     "moe_turnstile_destroy": (c_int, [c_void_p]),
     "moe_turnstile_set_span": (c_int, [c_void_p, c_int32]),
@@ -385,6 +426,106 @@ def moe_balance_loss_backward(logits, logits_dtype: int, logits_stride: int, tok
     return _lib.moe_balance_loss_backward(_ptr(logits), logits_dtype, logits_stride, _ptr(token_mask),
                                           _ptr(seq_offsets), S, T, E, k, coef, _ptr(counts), _ptr(live), _ptr(grad),
                                           _ptr(dlogits), dlogits_stride, int(bool(accumulate)), _stream(stream))
+
+
+# ---- the gated feed-forward block and its backward pass (include/moepd_ffn.h) ----
+
+
+def moe_ffn_gate_up(x, x_stride: int, rows: int, w_gate_up, groups: int, offsets, hidden: int, inter: int, dtype: int,
+                    gate_up, h, stream) -> int:
+    return _lib.moe_ffn_gate_up(_ptr(x), x_stride, rows, _ptr(w_gate_up), groups, _ptr(offsets), hidden, inter, dtype,
+                                _ptr(gate_up), _ptr(h), _stream(stream))
+
+
+def moe_ffn_down(h, rows: int, w_down, groups: int, offsets, hidden: int, inter: int, dtype: int, y, y_dtype: int,
+                 y_stride: int, stream) -> int:
+    return _lib.moe_ffn_down(_ptr(h), rows, _ptr(w_down), groups, _ptr(offsets), hidden, inter, dtype, _ptr(y), y_dtype,
+                             y_stride, _stream(stream))
+
+
+def moe_ffn_down_backward(dy, dy_stride: int, rows: int, w_down, gate_up, groups: int, offsets, hidden: int, inter: int,
+                          dtype: int, dgate_up, h, stream) -> int:
+    return _lib.moe_ffn_down_backward(_ptr(dy), dy_stride, rows, _ptr(w_down), _ptr(gate_up), groups, _ptr(offsets),
+                                      hidden, inter, dtype, _ptr(dgate_up), _ptr(h), _stream(stream))
+
+
+def moe_ffn_gate_up_backward(dgate_up, rows: int, w_gate_up, groups: int, offsets, hidden: int, inter: int, dtype: int, dx,
+                             dx_dtype: int, dx_stride: int, stream) -> int:
+    return _lib.moe_ffn_gate_up_backward(_ptr(dgate_up), rows, _ptr(w_gate_up), groups, _ptr(offsets), hidden, inter,
+                                         dtype, _ptr(dx), dx_dtype, dx_stride, _stream(stream))
+
+
+def moe_ffn_weight_workspace(rows: int, groups: int, m: int, n: int):
+    """(status, bytes)"""
+    b = c_int64()
+    st = _lib.moe_ffn_weight_workspace(rows, groups, m, n, byref(b))
+    return st, b.value
+
+
+def moe_ffn_weight_grad(a, a_stride: int, b, b_stride: int, rows: int, groups: int, offsets, m: int, n: int, dtype: int, dw,
+                        dw_dtype: int, accumulate: bool, workspace, workspace_bytes: int, stream) -> int:
+    return _lib.moe_ffn_weight_grad(_ptr(a), a_stride, _ptr(b), b_stride, rows, groups, _ptr(offsets), m, n, dtype,
+                                    _ptr(dw), dw_dtype, int(bool(accumulate)), _ptr(workspace), workspace_bytes,
+                                    _stream(stream))
+
+
+# ---- token rows there and back (include/moepd_rows.h) ----
+
+
+def moe_rows_gather(x, dtype: int, x_stride: int, T: int, token_of_row, row_count, rows: int, hidden: int, out,
+                    out_stride: int, stream) -> int:
+    return _lib.moe_rows_gather(_ptr(x), dtype, x_stride, T, _ptr(token_of_row), _ptr(row_count), rows, hidden, _ptr(out),
+                                out_stride, _stream(stream))
+
+
+def moe_rows_combine(y, y_dtype: int, y_stride: int, rows: int, w, row_of_slot, T: int, k: int, hidden: int, out,
+                     out_dtype: int, out_stride: int, stream) -> int:
+    return _lib.moe_rows_combine(_ptr(y), y_dtype, y_stride, rows, _ptr(w), _ptr(row_of_slot), T, k, hidden, _ptr(out),
+                                 out_dtype, out_stride, _stream(stream))
+
+
+def moe_rows_combine_backward(dout, dout_dtype: int, dout_stride: int, y, y_dtype: int, y_stride: int, rows: int, w,
+                              row_of_slot, T: int, k: int, hidden: int, dy, dy_dtype: int, dy_stride: int, dw,
+                              stream) -> int:
+    return _lib.moe_rows_combine_backward(_ptr(dout), dout_dtype, dout_stride, _ptr(y), y_dtype, y_stride, rows, _ptr(w),
+                                          _ptr(row_of_slot), T, k, hidden, _ptr(dy), dy_dtype, dy_stride, _ptr(dw),
+                                          _stream(stream))
+
+
+def moe_gate_backward(topk_idx, topk_w, dw, T: int, E: int, k: int, dlogits, dlogits_dtype: int, dlogits_stride: int,
+                      accumulate: bool, stream) -> int:
+    return _lib.moe_gate_backward(_ptr(topk_idx), _ptr(topk_w), _ptr(dw), T, E, k, _ptr(dlogits), dlogits_dtype,
+                                  dlogits_stride, int(bool(accumulate)), _stream(stream))
+
+
+# ---- AdamW (include/moepd_adamw.h) ----
+
+
+def adamw_tensor(param, param_dtype: int, master, grad, grad_dtype: int, m, v, m_scales, v_scales, n: int,
+                 weight_decay: float = 0.0) -> moe_adamw_tensor_t:
+    return moe_adamw_tensor_t(_ptr(param), _ptr(master), _ptr(grad), _ptr(m), _ptr(v), _ptr(m_scales), _ptr(v_scales), n,
+                              weight_decay, param_dtype, grad_dtype)
+
+
+def moe_adamw_create(tensors, state_bits: int):
+    """tensors: a sequence of adamw_tensor(...), or None.  (status, table)"""
+    out = c_void_p()
+    count = 0 if tensors is None else len(tensors)
+    arr = None if tensors is None else (moe_adamw_tensor_t * max(count, 1))(*tensors)
+    st = _lib.moe_adamw_create(arr, count, state_bits, byref(out))
+    return st, out.value
+
+
+def moe_adamw_step(table, beta1: float, beta2: float, eps: float, lr, step, grad_scale, seed: int, stream) -> int:
+    return _lib.moe_adamw_step(table, beta1, beta2, eps, _ptr(lr), _ptr(step), _ptr(grad_scale), seed, _stream(stream))
+
+
+def moe_adamw_read(table, index: int, m, root_v, dtype: int, stream) -> int:
+    return _lib.moe_adamw_read(table, index, _ptr(m), _ptr(root_v), dtype, _stream(stream))
+
+
+def moe_adamw_destroy(table) -> int:
+    return _lib.moe_adamw_destroy(table)
 
 
 # ---- turnstile (include/moepd_turnstile.h) ----
