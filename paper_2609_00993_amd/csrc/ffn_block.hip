@@ -16,7 +16,7 @@ namespace {
 
 __device__ __forceinline__ bool ffn_row_tile(const FfnArgs& g, int bm, int bn, FfnTile& t) {
   GroupTile w;
-  if (!group_tile<false>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), bm, w)) return false;
+  if (!group_tile<false, true>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), bm, w)) return false;
   t.group = w.group;
   t.m0 = w.m0;
   t.rows = w.m_end - w.m0;
@@ -25,23 +25,33 @@ __device__ __forceinline__ bool ffn_row_tile(const FfnArgs& g, int bm, int bn, F
   return true;
 }
 
-// Tiles of up to 160 rows, cut to the 32-row blocks that they hold; four waves side by side
-// along the columns.
-constexpr int kFfnMidRows = 160;
+// Tiles cut to the 32-row blocks that they hold; four waves side by side along the columns.
+constexpr int kFfnMidRows = 160, kFfnWideRows = 256;
 template <int KIND, bool F32>
 __global__ __launch_bounds__(256) void ffn_block_mid(FfnArgs g) {
-  __shared__ u32x4 lds[ffn_chunks(kFfnMidRows, 256, 3, 3)];
+  __shared__ u32x4 lds[ffn_chunks(kFfnMidRows, 256, 64, 3, 3)];
   FfnTile t;
   if (!ffn_row_tile(g, kFfnMidRows, KIND == kFfnGateUp ? 128 : 256, t)) return;
   const int blocks = (t.rows + 31) / 32;
-  if (blocks <= 1) ffn_tile<KIND, F32, 32, 256, 1, 4, 3, 3>(g, t, g.c, lds);
-  else if (blocks == 2) ffn_tile<KIND, F32, 64, 256, 1, 4, 3, 3>(g, t, g.c, lds);
-  else if (blocks == 3) ffn_tile<KIND, F32, 96, 256, 1, 4, 3, 3>(g, t, g.c, lds);
-  else if (blocks == 4) ffn_tile<KIND, F32, 128, 256, 1, 4, 3, 3>(g, t, g.c, lds);
-  else ffn_tile<KIND, F32, 160, 256, 1, 4, 3, 3>(g, t, g.c, lds);
+  if (blocks <= 1) ffn_tile<KIND, F32, 32, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
+  else if (blocks == 2) ffn_tile<KIND, F32, 64, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
+  else if (blocks == 3) ffn_tile<KIND, F32, 96, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
+  else if (blocks == 4) ffn_tile<KIND, F32, 128, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
+  else ffn_tile<KIND, F32, 160, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
+}
+
+// Groups of many rows: 256 rows, a 2 x 2 grid of waves, the rows' slices one ahead of the weights'.
+template <int KIND, bool F32>
+__global__ __launch_bounds__(256) void ffn_block_wide(FfnArgs g) {
+  __shared__ u32x4 lds[ffn_chunks(kFfnWideRows, 256, 64, 3, 2)];
+  FfnTile t;
+  if (!ffn_row_tile(g, kFfnWideRows, KIND == kFfnGateUp ? 128 : 256, t)) return;
+  ffn_tile<KIND, F32, 256, 256, 64, 2, 2, 3, 2>(g, t, g.c, lds);
 }
 
 // ------------------------------------------------------------------ gradients of the weights
+
+constexpr int kFfnWeightRows = 128, kFfnWeightCols = 256;
 
 // Workgroup b's tile: parts of the rows outermost, then groups; within a group blocks of four
 // column tiles, row tile by row tile; runs of consecutive tiles dealt to the XCDs in turn.
@@ -66,7 +76,7 @@ __device__ __forceinline__ bool ffn_weight_tile(const FfnArgs& g, int bm, int bn
     hi = uniform(max(lo, min(g.offsets[t.group + 1], g.rows)));
   }
   const int part = (hi - lo + g.splits - 1) / g.splits;
-  const int each = (part + kFfnSlice - 1) / kFfnSlice * kFfnSlice;
+  const int each = (part + 63) / 64 * 64;
   t.k0 = min((long long)hi, lo + (long long)split * each);
   t.k_count = min(each, hi - t.k0);
   return true;
@@ -74,12 +84,12 @@ __device__ __forceinline__ bool ffn_weight_tile(const FfnArgs& g, int bm, int bn
 
 template <bool F32>
 __global__ __launch_bounds__(256, 2) void ffn_block_weights(FfnArgs g) {
-  __shared__ u32x4 lds[ffn_chunks(128, 128, 2, 2)];
+  __shared__ u32x4 lds[ffn_chunks(kFfnWeightRows, kFfnWeightCols, 32, 3, 3)];
   FfnTile t;
   int split;
-  if (!ffn_weight_tile(g, 128, 128, t, split)) return;
+  if (!ffn_weight_tile(g, kFfnWeightRows, kFfnWeightCols, t, split)) return;
   uint8_t* c = g.c + ((long long)split * g.groups + t.group) * g.m * g.ldc;
-  ffn_tile<kFfnWeightGrad, F32, 128, 128, 2, 2, 2, 2>(g, t, c, lds);
+  ffn_tile<kFfnWeightGrad, F32, kFfnWeightRows, kFfnWeightCols, 32, 2, 2, 3, 3>(g, t, c, lds);
 }
 
 // The parts' sums, in order, to the result.
@@ -142,21 +152,30 @@ int launch_rows(FfnArgs g, int kind, bool out_f32, bool f32, hipStream_t s) {
     return launched() ? MOE_OK : MOE_ERR_HIP;
   }
   const int bn = kind == kFfnGateUp ? 128 : 256;
+  const bool wide = g.rows / g.groups >= 2 * kFfnWideRows;
   g.n_tiles = (g.n + bn - 1) / bn;
   g.run = 32;
-  const long long tiles = (g.rows / kFfnMidRows + (long long)g.groups) * g.n_tiles;
+  const long long tiles = (g.rows / (wide ? kFfnWideRows : kFfnMidRows) + (long long)g.groups) * g.n_tiles;
   if (tiles > kMostBlocks) return MOE_ERR_INVALID_ARG;
   const dim3 grid = grid_of((tiles + 7) / 8 * 8, 256);
+  auto go = [&](auto kind_of, auto f32_of) {
+    constexpr int KIND = decltype(kind_of)::value;
+    constexpr bool F32 = decltype(f32_of)::value;
+    if (wide) ffn_block_wide<KIND, F32><<<grid, 256, 0, s>>>(g);
+    else ffn_block_mid<KIND, F32><<<grid, 256, 0, s>>>(g);
+  };
+  using No = std::false_type;
+  using Yes = std::true_type;
   switch (kind) {
-    case kFfnGateUp: ffn_block_mid<kFfnGateUp, false><<<grid, 256, 0, s>>>(g); break;
+    case kFfnGateUp: go(std::integral_constant<int, kFfnGateUp>{}, No{}); break;
     case kFfnDown:
-      if (out_f32) ffn_block_mid<kFfnDown, true><<<grid, 256, 0, s>>>(g);
-      else ffn_block_mid<kFfnDown, false><<<grid, 256, 0, s>>>(g);
+      if (out_f32) go(std::integral_constant<int, kFfnDown>{}, Yes{});
+      else go(std::integral_constant<int, kFfnDown>{}, No{});
       break;
-    case kFfnDownGrad: ffn_block_mid<kFfnDownGrad, false><<<grid, 256, 0, s>>>(g); break;
+    case kFfnDownGrad: go(std::integral_constant<int, kFfnDownGrad>{}, No{}); break;
     default:
-      if (out_f32) ffn_block_mid<kFfnGateUpGrad, true><<<grid, 256, 0, s>>>(g);
-      else ffn_block_mid<kFfnGateUpGrad, false><<<grid, 256, 0, s>>>(g);
+      if (out_f32) go(std::integral_constant<int, kFfnGateUpGrad>{}, Yes{});
+      else go(std::integral_constant<int, kFfnGateUpGrad>{}, No{});
   }
   return launched() ? MOE_OK : MOE_ERR_HIP;
 }
@@ -188,12 +207,14 @@ int size_of(int32_t dtype) { return dtype == MOE_DTYPE_F32 ? 4 : 2; }
 // Parts of the rows for the weights' gradient: enough tiles to fill the GPU twice, and at
 // least four slices to a part.  128 x 128 tiles of 64 KB: 512 of them are 2^25 bytes.
 int weight_splits(long long rows, int groups, long long tiles) {
-  const long long slices = rows / groups / kFfnSlice;
+  const long long slices = rows / groups / 64;
   long long s = (512 + tiles - 1) / tiles;
   s = s < slices / 4 ? s : slices / 4;
   return tiles >= 384 || s < 2 ? 1 : (int)s;
 }
-long long weight_tiles(int groups, int m, int n) { return (long long)groups * ((m + 127) / 128) * ((n + 127) / 128); }
+long long weight_tiles(int groups, int m, int n) { 
+  return (long long)groups * ((m + kFfnWeightRows - 1) / kFfnWeightRows) * ((n + kFfnWeightCols - 1) / kFfnWeightCols);
+}
 long long weight_bytes(long long rows, int groups, int m, int n) {
   const int s = weight_splits(rows, groups, weight_tiles(groups, m, n));
   return s > 1 ? 4LL * s * groups * m * n : 0;
@@ -339,14 +360,15 @@ int moe_ffn_weight_grad(const void* a, int64_t a_stride, const void* b, int64_t 
   g.groups = groups;
   g.m = m;
   g.n = n;
-  g.run = 32;
+  g.run = 64;
   g.splits = need > 0 ? weight_splits(rows, groups, weight_tiles(groups, m, n)) : 1;
   g.c = g.splits > 1 ? (uint8_t*)workspace : (uint8_t*)dw;
   g.accumulate = g.splits > 1 ? 0 : accumulate != 0;
   g.ldc = (long long)n * (g.splits > 1 ? 4 : size_of(dw_dtype));
-  const int edge = dtype == MOE_DTYPE_F32 ? kFfnF32Rows : 128;
-  g.m_tiles = (m + edge - 1) / edge;
-  g.n_tiles = (n + edge - 1) / edge;
+  const int bm = dtype == MOE_DTYPE_F32 ? kFfnF32Rows : kFfnWeightRows;
+  const int bn = dtype == MOE_DTYPE_F32 ? kFfnF32Cols : kFfnWeightCols;
+  g.m_tiles = (m + bm - 1) / bm;
+  g.n_tiles = (n + bn - 1) / bn;
   const long long tiles = (long long)g.m_tiles * g.n_tiles * groups * g.splits;
   if (tiles > kMostBlocks) return MOE_ERR_INVALID_ARG;
   const dim3 grid = grid_of((tiles + 7) / 8 * 8, 256);

@@ -8,7 +8,7 @@
 //   gate/up grad  a = dgate_up by rows,  b = w_gate_up by columns (k = 2I)
 //   weights' grad a, b by columns (k = the group's rows)
 //
-// A slice is 64 of K.  Slices travel HBM -> LDS by 16-byte DMA into rings, and the
+// A slice is BK (32 or 64) of K.  Slices travel HBM -> LDS by 16-byte DMA into rings, and the
 // 32x32x16 MFMA's operands (lane l: row l % 32, 8 values of k from 8 (l / 32) on) are read
 // from there: by rows with one ds_read_b128, whose 16-byte chunks are swizzled by the row
 // (swz in pipeline.h); by columns with two ds_read_b64_tr_b16, each of which gives a
@@ -69,7 +69,6 @@ struct FfnTile {  // wave-uniform
 
 __device__ __forceinline__ bf16x8_ffn as_bf16x8_ffn(const u32x4& u) { return __builtin_bit_cast(bf16x8_ffn, u); }
 
-constexpr int kFfnSlice = 64;       // K of a slice
 constexpr int kFfnNowhere = 1 << 30;  // past every resource: bytes of an operand panel stay below it
 
 // Four rows x 16 columns per 16 lanes, transposed: lane i gives row i / 4, columns 4 (i % 4)
@@ -82,14 +81,14 @@ __device__ __forceinline__ i16x4_ffn ffn_read_tr(ffn_lds_ptr __restrict__ at) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16(at);
 }
 
-// One operand's part of a slice in LDS: P rows of 64 values, or 64 rows of P values.
-template <bool COL, int P>
+// One operand's part of a slice in LDS: P rows of BK values, or BK rows of P values.
+template <bool COL, int P, int BK>
 struct FfnPanel {
-  static constexpr int CPR = COL ? P / 8 : kFfnSlice / 8;   // 16-byte chunks of an LDS row
-  static constexpr int RPI = 64 / CPR;                      // LDS rows of one DMA instruction (1 KB)
-  static constexpr int CH = P * kFfnSlice / 8;              // chunks of a slice
-  static constexpr int INS = CH / 64 / 4;                   // DMA instructions of a wave and slice
-  static_assert(INS * 4 * 64 == CH && (!COL || P == 128 || P == 256), "whole instructions");
+  static constexpr int CPR = COL ? P / 8 : BK / 8;  // 16-byte chunks of an LDS row
+  static constexpr int RPI = 64 / CPR;              // LDS rows of one DMA instruction (1 KB)
+  static constexpr int CH = P * BK / 8;             // chunks of a slice
+  static constexpr int INS = (CH / 64 + 3) / 4;     // DMA instructions of a wave and slice
+  static_assert(CH % 64 == 0 && (!COL || P == 128 || P == 256), "whole instructions");
 
   uint8_t* base;  // by rows: of the panel's first row; by columns: of row 0, at the panel's first column
   long long ld;
@@ -99,6 +98,13 @@ struct FfnPanel {
   int tail;       // by rows: bit i: this lane's chunk of instruction i is past K in the last slice
   int off[INS];   // this lane's byte of instruction i
 
+  // The waves take the slice's instructions in turn; where these do not go round, the last ones
+  // are issued twice (the same bytes to the same place), so that every wave counts alike.
+  static __device__ __forceinline__ int instruction(int i, int wave) {
+    const int n = 4 * i + wave;
+    if constexpr (CH / 64 % 4 == 0) return n;
+    return n < CH / 64 ? n : n - CH / 64 % 4;
+  }
   // row_of(r): the panel's row r in the resource that starts at `first`.
   template <class F>
   __device__ __forceinline__ void by_rows(const uint8_t* first, long long stride, int nbytes, int k, int wave, int lane,
@@ -107,11 +113,11 @@ struct FfnPanel {
     ld = stride;
     bytes = uniform(nbytes);
     tail = 0;
-    const int last = (k - 1) / kFfnSlice * kFfnSlice;
+    const int last = (k - 1) / BK * BK;
 #pragma unroll
     for (int i = 0; i < INS; ++i) {
-      const int r = (wave * INS + i) * RPI + lane / CPR;
-      const int chunk = (lane % CPR) ^ swz<kFfnSlice>(r);
+      const int r = instruction(i, wave) * RPI + lane / CPR;
+      const int chunk = (lane % CPR) ^ swz<BK>(r);
       off[i] = row_of(r) * (int)stride + chunk * 16;
       tail |= (last + 8 * chunk >= k ? 1 : 0) << i;
     }
@@ -124,22 +130,22 @@ struct FfnPanel {
     width = uniform(columns * 2);
 #pragma unroll
     for (int i = 0; i < INS; ++i) {
-      const int r = (wave * INS + i) * RPI + lane / CPR;
+      const int r = instruction(i, wave) * RPI + lane / CPR;
       off[i] = r * (int)stride + ((lane % CPR) ^ (4 * (r & 3))) * 16;
     }
   }
   __device__ __forceinline__ void issue(int i, int kt, bool last, u32x4* slot, int wave) const {
-    u32x4* dst = slot + (wave * INS + i) * 64;
+    u32x4* dst = slot + instruction(i, wave) * 64;
     if constexpr (COL) {
       // a resource of the slice's rows: past them, and past the last one's columns, zeros
-      const int n = (min(left - kt * kFfnSlice, kFfnSlice) - 1) * (int)ld + width;
+      const int n = (min(left - kt * BK, BK) - 1) * (int)ld + width;
       const __amdgpu_buffer_rsrc_t rsrc =
-          __builtin_amdgcn_make_buffer_rsrc(base + (long long)kt * kFfnSlice * ld, (short)0, n, kBufferRsrcWord3);
+          __builtin_amdgcn_make_buffer_rsrc(base + (long long)kt * BK * ld, (short)0, n, kBufferRsrcWord3);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, MOEPD_LPTR(dst), 16, off[i], 0, 0, 0);
     } else {
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(base, (short)0, bytes, kBufferRsrcWord3);
       const int past = ((tail & -(int)last) >> i) & 1;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, MOEPD_LPTR(dst), 16, off[i] | past * kFfnNowhere, kt * (2 * kFfnSlice), 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, MOEPD_LPTR(dst), 16, off[i] | past * kFfnNowhere, kt * (2 * BK), 0, 0);
     }
   }
   // The MFMA operand of 32 rows from row `p` (a multiple of 32) on, substep `sub` (16 of k).
@@ -153,7 +159,7 @@ struct FfnPanel {
       return __builtin_bit_cast(bf16x8_ffn, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
       const int r = p + (lane & 31);
-      return as_bf16x8_ffn(slot[r * CPR + ((2 * sub + (lane >> 5)) ^ swz<kFfnSlice>(r))]);
+      return as_bf16x8_ffn(slot[r * CPR + ((2 * sub + (lane >> 5)) ^ swz<BK>(r))]);
     }
   }
 };
@@ -168,6 +174,10 @@ __device__ __forceinline__ void ffn_unpack8(const u32x4& q, float (&v)[8]) {
     v[2 * i] = __uint_as_float(q[i] << 16);
     v[2 * i + 1] = __uint_as_float(q[i] & 0xffff0000u);
   }
+}
+
+__device__ __forceinline__ void ffn_store16(uint8_t* p, const u32x4& v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
 }
 
 // What 8 neighbouring results of one row become.  Where(row) gives places, load() what
@@ -231,27 +241,27 @@ struct FfnStore {
         }
       }
       if constexpr (F32) {
-        store16(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
-        store16(p + 16, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+        ffn_store16(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+        ffn_store16(p + 16, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
       } else {
-        store16(p, ffn_bf16x8(v));
+        ffn_store16(p, ffn_bf16x8(v));
       }
     }
   }
 };
 
-// LDS of a tile, in 16-byte chunks: SA slots of the BM x 64 panel, SB of the BR x 64 one.
-constexpr int ffn_chunks(int bm, int br, int sa, int sb) { return (sa * bm + sb * br) * (kFfnSlice / 8); }
+// LDS of a tile, in 16-byte chunks: SA slots of the BM x BK panel, SB of the BR x BK one.
+constexpr int ffn_chunks(int bm, int br, int bk, int sa, int sb) { return (sa * bm + sb * br) * (bk / 8); }
 
 // A tile of BM rows and BR columns (gate/up: BR / 2 of each), by a WM x WN grid of waves.
-template <int KIND, bool F32, int BM, int BR, int WM, int WN, int SA, int SB>
+template <int KIND, bool F32, int BM, int BR, int BK, int WM, int WN, int SA, int SB>
 __device__ __forceinline__ void ffn_tile(const FfnArgs& g, const FfnTile& t, uint8_t* c, u32x4* lds) {
   constexpr bool GATED = KIND == kFfnGateUp, A_COL = KIND == kFfnWeightGrad, B_COL = KIND >= kFfnDownGrad;
   constexpr int NB = GATED ? 2 : 1, BN = BR / NB;
   constexpr int WTM = BM / WM, WTN = BN / WN, FM = WTM / 32, FN = WTN / 32, FB = FN * NB;
-  constexpr int SUB = kFfnSlice / 16, NRD = FM + FB, NMF = FM * FB;
-  using PA = FfnPanel<A_COL, BM>;
-  using PB = FfnPanel<B_COL, BR>;
+  constexpr int SUB = BK / 16, NRD = FM + FB, NMF = FM * FB;
+  using PA = FfnPanel<A_COL, BM, BK>;
+  using PB = FfnPanel<B_COL, BR, BK>;
   constexpr int A_INS = PA::INS, B_INS = PB::INS, NPS = A_INS + B_INS;
   constexpr int LEAD = SA - SB;
   static_assert(WM * WN == 4 && FM * 32 == WTM && FN * 32 == WTN, "four waves of whole blocks");
@@ -266,7 +276,7 @@ __device__ __forceinline__ void ffn_tile(const FfnArgs& g, const FfnTile& t, uin
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
   const int K = KIND == kFfnWeightGrad ? t.k_count : g.k;
-  const int KT = (K + kFfnSlice - 1) / kFfnSlice;
+  const int KT = (K + BK - 1) / BK;
 
   PA pa;
   PB pb;
@@ -285,8 +295,22 @@ __device__ __forceinline__ void ffn_tile(const FfnArgs& g, const FfnTile& t, uin
       return GATED && r >= BN ? g.n + min(t.n0 + r - BN, g.n - 1) : min(t.n0 + r, g.n - 1);
     });
 
-  auto issue_a1 = [&](int i, int kt, int slot) { pa.issue(i, kt, kt == KT - 1, ring_a + slot * PA::CH, wave); };
-  auto issue_b1 = [&](int i, int kt, int slot) { pb.issue(i, kt, kt == KT - 1, ring_b + slot * PB::CH, wave); };
+  // Where weights by rows are a multiple of 4 KB apart, they all start on one memory channel, and
+  // tiles that read the same k at a time press on a few: the tiles of a column tile start at
+  // their own slice, and go round.
+  int rot = 0;
+  if constexpr (!B_COL) {
+    if (g.ldb % 4096 == 0) rot = uniform((int)((unsigned)(t.group * g.n_tiles + t.n0 / BN) * 2u % (unsigned)KT));
+  }
+  auto slice_at = [&](int kt) { return B_COL || kt + rot < KT ? kt + rot : kt + rot - KT; };
+  auto issue_a1 = [&](int i, int kt, int slot) {
+    const int at = slice_at(kt);
+    pa.issue(i, at, at == KT - 1, ring_a + slot * PA::CH, wave);
+  };
+  auto issue_b1 = [&](int i, int kt, int slot) {
+    const int at = slice_at(kt);
+    pb.issue(i, at, at == KT - 1, ring_b + slot * PB::CH, wave);
+  };
   auto issue_a = [&](int kt, int slot) {
 #pragma unroll
     for (int i = 0; i < A_INS; ++i) issue_a1(i, kt, slot);
@@ -425,7 +449,7 @@ __device__ __forceinline__ void ffn_tile(const FfnArgs& g, const FfnTile& t, uin
   // beyond their width, read back 8 columns of a row to a lane, so that memory sees whole
   // lines and the elementwise part works on 16-byte vectors.
   constexpr int PITCH = WTN + 4, PATCH = 32 * PITCH;  // floats
-  static_assert(4 * NB * PATCH <= 4 * ffn_chunks(BM, BR, SA, SB), "patches within the ring");
+  static_assert(4 * NB * PATCH <= 4 * ffn_chunks(BM, BR, BK, SA, SB), "patches within the ring");
   float* patch = reinterpret_cast<float*>(lds) + wave * (NB * PATCH);
   constexpr int LPR = WTN / 8, RPP = 64 / LPR, PASSES = 32 / RPP;
   using Out = FfnStore<KIND, F32>;

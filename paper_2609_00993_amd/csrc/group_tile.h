@@ -42,7 +42,8 @@ __device__ __forceinline__ int wave_scan(int v) {
 // XCD b % 8, so the row tiles that read one weight panel share an L2, and every XCD
 // streams an eighth of every group's weights.
 //
-// Otherwise (ring tiles): a group's rows are shared evenly among its row tiles; its
+// Otherwise (ring tiles): a group's rows are shared evenly among its row tiles (BLOCKS: its
+// blocks of 32 rows are, for tiles cut to them); its
 // tiles run over blocks of four column tiles, in each row tile by row tile; and runs of
 // consecutive tiles are dealt to the XCDs in turn, so that an XCD's L2 serves each row
 // block to four workgroups and each weight panel to as many as the run has row
@@ -50,7 +51,7 @@ __device__ __forceinline__ int wave_scan(int v) {
 // (16 row x 4 column tiles: what an XCD's CUs hold at a time) for groups of many rows,
 // else 32, which leave less to the last round: 96,889 skewed rows (7168 x 2048)
 // 1030 us with 64, 1096 with 32; 32,768 rows 391 / 430; 8192 rows, 256 to a group, 77 / 73.
-template <bool STRIPED, class G>
+template <bool STRIPED, bool BLOCKS = false, class G>
 __device__ __forceinline__ bool group_tile(const G& g, int b, int bm, GroupTile& t) {
   const int lane = lane_id();
   int l = 0, h = 0, mt = 0, incl = 0;  // of group g0 + lane
@@ -106,9 +107,15 @@ __device__ __forceinline__ bool group_tile(const G& g, int b, int bm, GroupTile&
     const int width = min(4, g.n_tiles - 4 * q);
     const int mi = r / width;
     t.nt = uniform(4 * q + r - mi * width);
-    const int per = (hi - lo + mt_e - 1) / mt_e;
-    t.m0 = uniform(lo + mi * per);
-    t.m_end = uniform(min(t.m0 + per, hi));
+    if constexpr (BLOCKS) {
+      const int nb = (hi - lo + 31) / 32;
+      t.m0 = uniform(lo + (int)((long long)nb * mi / mt_e) * 32);
+      t.m_end = uniform(min(lo + (int)((long long)nb * (mi + 1) / mt_e) * 32, hi));
+    } else {
+      const int per = (hi - lo + mt_e - 1) / mt_e;
+      t.m0 = uniform(lo + mi * per);
+      t.m_end = uniform(min(t.m0 + per, hi));
+    }
   }
   return true;
 }
