@@ -1,5 +1,6 @@
 // The gated feed-forward block and its backward pass (include/moepd_ffn.h): tiles, launches and
 // the C entry points.  The tile itself is in ffn_ring.h (bf16) and ffn_block_f32.h.
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -26,12 +27,11 @@ __device__ __forceinline__ bool ffn_row_tile(const FfnArgs& g, int bm, int bn, F
 }
 
 // Tiles cut to the 32-row blocks that they hold; four waves side by side along the columns.
-constexpr int kFfnMidRows = 160, kFfnWideRows = 256;
 template <int KIND, bool F32>
 __global__ __launch_bounds__(256) void ffn_block_mid(FfnArgs g) {
   __shared__ u32x4 lds[ffn_chunks(kFfnMidRows, 256, 64, 3, 3)];
   FfnTile t;
-  if (!ffn_row_tile(g, kFfnMidRows, KIND == kFfnGateUp ? 128 : 256, t)) return;
+  if (!ffn_row_tile(g, g.bm, KIND == kFfnGateUp ? 128 : 256, t)) return;
   const int blocks = (t.rows + 31) / 32;
   if (blocks <= 1) ffn_tile<KIND, F32, 32, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
   else if (blocks == 2) ffn_tile<KIND, F32, 64, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
@@ -47,6 +47,16 @@ __global__ __launch_bounds__(256) void ffn_block_wide(FfnArgs g) {
   FfnTile t;
   if (!ffn_row_tile(g, kFfnWideRows, KIND == kFfnGateUp ? 128 : 256, t)) return;
   ffn_tile<KIND, F32, 256, 256, 64, 2, 2, 3, 2>(g, t, g.c, lds);
+}
+
+// Few rows: up to 8 by eight waves of two blocks in flight each, up to 32 by four of three.
+template <int KIND, bool F32, int RA>
+__global__ __launch_bounds__(RA == 8 ? 512 : 256) void ffn_block_few(FfnArgs g) {
+  constexpr int NB = KIND == kFfnDown ? 1 : 2, W = RA == 8 ? 8 : 4, S = RA == 8 ? (NB == 1 ? 3 : 2) : 3;
+  __shared__ u32x4 lds[ffn_few_chunks(RA, NB, W, S)];
+  FfnTile t;
+  if (!ffn_row_tile(g, RA, KIND == kFfnGateUp ? 32 : 32 * NB, t)) return;
+  ffn_few_tile<KIND, F32, RA, NB, W, S>(g, t, lds);
 }
 
 // ------------------------------------------------------------------ gradients of the weights
@@ -151,18 +161,21 @@ int launch_rows(FfnArgs g, int kind, bool out_f32, bool f32, hipStream_t s) {
     }
     return launched() ? MOE_OK : MOE_ERR_HIP;
   }
-  const int bn = kind == kFfnGateUp ? 128 : 256;
-  const bool wide = g.rows / g.groups >= 2 * kFfnWideRows;
-  g.n_tiles = (g.n + bn - 1) / bn;
-  g.run = 32;
-  const long long tiles = (g.rows / (wide ? kFfnWideRows : kFfnMidRows) + (long long)g.groups) * g.n_tiles;
-  if (tiles > kMostBlocks) return MOE_ERR_INVALID_ARG;
-  const dim3 grid = grid_of((tiles + 7) / 8 * 8, 256);
+  const FfnForm f = ffn_form(kind, g.rows, g.groups, g.n, g.k);
+  if (f.count > kMostBlocks) return MOE_ERR_INVALID_ARG;
+  g.bm = f.rows;
+  g.n_tiles = f.n_tiles;
+  g.run = f.run;
+  const dim3 grid = grid_of((f.count + 7) / 8 * 8, f.threads());
   auto go = [&](auto kind_of, auto f32_of) {
     constexpr int KIND = decltype(kind_of)::value;
     constexpr bool F32 = decltype(f32_of)::value;
-    if (wide) ffn_block_wide<KIND, F32><<<grid, 256, 0, s>>>(g);
-    else ffn_block_mid<KIND, F32><<<grid, 256, 0, s>>>(g);
+    switch (f.tiles) {
+      case kFfnFew8: ffn_block_few<KIND, F32, 8><<<grid, f.threads(), 0, s>>>(g); break;
+      case kFfnFew32: ffn_block_few<KIND, F32, 32><<<grid, f.threads(), 0, s>>>(g); break;
+      case kFfnMid: ffn_block_mid<KIND, F32><<<grid, f.threads(), 0, s>>>(g); break;
+      default: ffn_block_wide<KIND, F32><<<grid, f.threads(), 0, s>>>(g);
+    }
   };
   using No = std::false_type;
   using Yes = std::true_type;
@@ -360,7 +373,6 @@ int moe_ffn_weight_grad(const void* a, int64_t a_stride, const void* b, int64_t 
   g.groups = groups;
   g.m = m;
   g.n = n;
-  g.run = 64;
   g.splits = need > 0 ? weight_splits(rows, groups, weight_tiles(groups, m, n)) : 1;
   g.c = g.splits > 1 ? (uint8_t*)workspace : (uint8_t*)dw;
   g.accumulate = g.splits > 1 ? 0 : accumulate != 0;
@@ -369,6 +381,9 @@ int moe_ffn_weight_grad(const void* a, int64_t a_stride, const void* b, int64_t 
   const int bn = dtype == MOE_DTYPE_F32 ? kFfnF32Cols : kFfnWeightCols;
   g.m_tiles = (m + bm - 1) / bm;
   g.n_tiles = (n + bn - 1) / bn;
+  // An eighth of a group's tiles to each XCD, so that groups of any length weigh on all alike, but
+  // no more than an XCD holds at a time.
+  g.run = std::min(std::max(g.m_tiles * g.n_tiles / 8, 4), 64);
   const long long tiles = (long long)g.m_tiles * g.n_tiles * groups * g.splits;
   if (tiles > kMostBlocks) return MOE_ERR_INVALID_ARG;
   const dim3 grid = grid_of((tiles + 7) / 8 * 8, 256);

@@ -1,0 +1,60 @@
+// Which tiles a product of the gated feed-forward block takes (ffn_block.hip), by sizes alone.  Plain
+// arithmetic, compiled for the host too, where a test asks for it.
+#pragma once
+
+namespace moepd {
+
+enum FfnKind : int { kFfnGateUp = 0, kFfnDown = 1, kFfnDownGrad = 2, kFfnGateUpGrad = 3, kFfnWeightGrad = 4 };
+
+// kFfnFew8, kFfnFew32: up to 8 or 32 rows and 32 or 64 columns, K dealt among the waves; kFfnMid: up to `rows`
+// (32 to 160) rows and 256 columns (gate/up: 128 of each), cut to the 32-row blocks they hold; kFfnWide: 256 rows.
+enum FfnTiles : int { kFfnFew8 = 0, kFfnFew32 = 1, kFfnMid = 2, kFfnWide = 3 };
+
+constexpr int kFfnMidRows = 160, kFfnWideRows = 256, kFfnCus = 256;
+
+struct FfnForm {
+  int tiles;          // FfnTiles
+  int rows, columns;  // of a tile at most
+  int run;            // consecutive tiles that go to one XCD
+  int n_tiles;
+  long long count;    // workgroups at most
+  int threads() const { return tiles == kFfnFew8 ? 512 : 256; }
+};
+
+// rows in `groups` groups, n columns, K values to a sum.  The times behind the rule, in ns with every CU at work:
+// a slice of 64 of K takes a mid tile 300 + 105 for each 32-row block, a wide one 1170, a few tile's start and
+// join 3000 and each value of K 2; mid and wide tiles start and end in 3000.  Measured, one group, us, mid / few: 128 rows, H
+// 7168, I 2048, gate/up 79 / 20, down 26 / 19; 512 rows, H 2048, I 1024, 46 / 14 and 24 / 14; 1000 rows, H 7168, I 2048,
+// gate/up 131 (wide) / 138, down 43 / 118; 500 rows there, mid tiles of 160 / 96 / 64 rows, 81 / 68 / 57.  32 groups of one
+// row, H 2560, I 768: gate/up 37 / 41.
+inline FfnForm ffn_form(int kind, long long rows, int groups, int n, int k) {
+  const long long touched = groups < rows ? groups : rows;  // groups that have a row, if shared evenly
+  const int mean = (int)((rows + touched - 1) / touched);
+  auto up = [](long long a, long long b) { return (a + b - 1) / b; };
+  FfnForm best{};
+  double least = 0;
+  auto consider = [&](int tiles, int bm, int bn, auto&& tile_ns) {
+    const int here = (int)up(mean, bm);  // row tiles of a group
+    const long long count = touched * here * up(n, bn);
+    const double rounds = count <= 4 * kFfnCus ? (double)up(count, kFfnCus) : (double)count / kFfnCus;
+    const double ns = rounds * tile_ns((int)up(up(mean, 32), here));
+    if (best.columns && ns >= least) return;
+    least = ns;
+    best.tiles = tiles;
+    best.rows = bm;
+    best.columns = bn;
+    best.n_tiles = (int)up(n, bn);
+    best.run = count >= 8 * 32 ? 32 : count >= 16 ? (int)(count / 8) : 2;
+    best.count = (rows / bm + touched) * best.n_tiles;
+  };
+  const int bn = kind == kFfnGateUp ? 128 : 256, few_bn = kind == kFfnGateUp || kind == kFfnDown ? 32 : 64;
+  const double slices = (double)up(k, 64);
+  if (mean >= 2 * kFfnWideRows) consider(kFfnWide, kFfnWideRows, bn, [&](int) { return 3000 + 1170 * slices; });
+  for (int bm = kFfnMidRows; bm >= 32; bm -= 32)
+    consider(kFfnMid, bm, bn, [&](int blocks) { return 3000 + (300 + 105 * blocks) * slices; });
+  const bool few8 = rows <= 8;
+  consider(few8 ? kFfnFew8 : kFfnFew32, few8 ? 8 : 32, few_bn, [&](int) { return 3000 + 2.0 * k; });
+  return best;
+}
+
+}  // namespace moepd

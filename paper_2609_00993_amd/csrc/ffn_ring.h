@@ -25,6 +25,7 @@
 // grouped GEMMs in ffn_bf16.hip (gemm_ring_body): see there.
 #pragma once
 
+#include "ffn_form.h"
 #include "group_tile.h"
 #include "pipeline.h"
 #include "swiglu.h"
@@ -36,8 +37,6 @@ typedef short i16x4_ffn __attribute__((ext_vector_type(4)));
 typedef short i16x8_ffn __attribute__((ext_vector_type(8)));
 typedef float f32x16_ffn __attribute__((ext_vector_type(16)));
 typedef float f32x4_ffn __attribute__((ext_vector_type(4)));
-
-enum FfnKind : int { kFfnGateUp = 0, kFfnDown = 1, kFfnDownGrad = 2, kFfnGateUpGrad = 3, kFfnWeightGrad = 4 };
 
 struct FfnArgs {
   const uint8_t* a;
@@ -55,6 +54,7 @@ struct FfnArgs {
   int m;           // weights' grad: rows of the result
   int n_tiles;     // column tiles; set by the launcher
   int m_tiles;     // weights' grad: row tiles; set by the launcher
+  int bm;          // rows of a tile at most; set by the launcher
   int run;         // consecutive tiles that go to one XCD; set by the launcher
   int splits;      // weights' grad: parts of a group's rows, each with a result of its own
   int accumulate;  // weights' grad: add to c
@@ -82,13 +82,16 @@ __device__ __forceinline__ i16x4_ffn ffn_read_tr(ffn_lds_ptr __restrict__ at) {
 }
 
 // One operand's part of a slice in LDS: P rows of BK values, or BK rows of P values.
-template <bool COL, int P, int BK>
+// Moved by SHARE waves.
+template <bool COL, int P, int BK, int SHARE = 4>
 struct FfnPanel {
   static constexpr int CPR = COL ? P / 8 : BK / 8;  // 16-byte chunks of an LDS row
   static constexpr int RPI = 64 / CPR;              // LDS rows of one DMA instruction (1 KB)
   static constexpr int CH = P * BK / 8;             // chunks of a slice
-  static constexpr int INS = (CH / 64 + 3) / 4;     // DMA instructions of a wave and slice
-  static_assert(CH % 64 == 0 && (!COL || P == 128 || P == 256), "whole instructions");
+  static constexpr int INS = (CH / 64 + SHARE - 1) / SHARE;  // DMA instructions of a wave and slice
+  static_assert(CH % 64 == 0 && (!COL || P == 64 || P == 128 || P == 256), "whole instructions");
+  // By columns: the 64-byte pieces of row k are swizzled by this (a row of 128 bytes has two).
+  static __device__ __forceinline__ int twist(int k) { return P == 64 ? (k >> 1) & 1 : k & 3; }
 
   uint8_t* base;  // by rows: of the panel's first row; by columns: of row 0, at the panel's first column
   long long ld;
@@ -101,9 +104,9 @@ struct FfnPanel {
   // The waves take the slice's instructions in turn; where these do not go round, the last ones
   // are issued twice (the same bytes to the same place), so that every wave counts alike.
   static __device__ __forceinline__ int instruction(int i, int wave) {
-    const int n = 4 * i + wave;
-    if constexpr (CH / 64 % 4 == 0) return n;
-    return n < CH / 64 ? n : n - CH / 64 % 4;
+    const int n = SHARE * i + wave;
+    if constexpr (CH / 64 % SHARE == 0) return n;
+    return n < CH / 64 ? n : n - CH / 64 % SHARE;
   }
   // row_of(r): the panel's row r in the resource that starts at `first`.
   template <class F>
@@ -131,7 +134,7 @@ struct FfnPanel {
 #pragma unroll
     for (int i = 0; i < INS; ++i) {
       const int r = instruction(i, wave) * RPI + lane / CPR;
-      off[i] = r * (int)stride + ((lane % CPR) ^ (4 * (r & 3))) * 16;
+      off[i] = r * (int)stride + ((lane % CPR) ^ (4 * twist(r))) * 16;
     }
   }
   __device__ __forceinline__ void issue(int i, int kt, bool last, u32x4* slot, int wave) const {
@@ -153,12 +156,12 @@ struct FfnPanel {
     if constexpr (COL) {
       const int g = lane >> 4, i = lane & 15;
       const uint8_t* at = reinterpret_cast<const uint8_t*>(slot) + (8 * (g >> 1) + (i >> 2)) * (P * 2) +
-                          ((p / 32) ^ (i >> 2)) * 64 + 32 * (g & 1) + 8 * (i & 3) + sub * (16 * P * 2);
+                          ((p / 32) ^ twist(i >> 2)) * 64 + 32 * (g & 1) + 8 * (i & 3) + sub * (16 * P * 2);
       const i16x4_ffn lo = ffn_read_tr((ffn_lds_ptr)(at));
       const i16x4_ffn hi = ffn_read_tr((ffn_lds_ptr)(at + 4 * P * 2));
       return __builtin_bit_cast(bf16x8_ffn, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      const int r = p + (lane & 31);
+      const int r = p + (lane & (P < 32 ? P - 1 : 31));
       return as_bf16x8_ffn(slot[r * CPR + ((2 * sub + (lane >> 5)) ^ swz<BK>(r))]);
     }
   }
@@ -487,6 +490,111 @@ __device__ __forceinline__ void ffn_tile(const FfnArgs& g, const FfnTile& t, uin
       if (row < t.rows && n_at < g.n) Out::store(g, t, c, row, n_at, old[p], v, up);
     }
     __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// A tile of up to 32 rows and 32 NB columns (gate/up: 32 of each) for few rows, where the stream of
+// weights is what bounds a product: the W waves of a workgroup deal the tile's blocks of 64 of K
+// among them, each with a ring of S blocks of its own (no barrier: a wave waits for its own
+// transfers alone), and their sums meet in LDS and are added in wave order.  Up to 8 rows take an
+// 8-row panel (RA), whose rows the MFMA's 32 read over and over: what the others give is not stored.
+constexpr int ffn_few_chunks(int ra, int nb, int w, int s) { return w * s * (ra + 32 * nb) * 8; }
+template <int KIND, bool F32, int RA, int NB, int W, int S>
+__device__ __forceinline__ void ffn_few_tile(const FfnArgs& g, const FfnTile& t, u32x4* lds) {
+  constexpr bool GATED = KIND == kFfnGateUp, B_COL = KIND >= kFfnDownGrad;
+  static_assert(KIND != kFfnWeightGrad && (!GATED || NB == 2) && (!B_COL || NB == 2), "panels");
+  constexpr int BN = GATED ? 32 : 32 * NB;
+  using PA = FfnPanel<false, RA, 64, 1>;
+  using PB = FfnPanel<B_COL, 32 * NB, 64, 1>;
+  constexpr int NP = PA::INS + PB::INS, SLOT = PA::CH + PB::CH;
+  static_assert(NP * S < 64, "wait range");
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  u32x4* ring = lds + wave * (S * SLOT);
+  const int KT = (g.k + 63) / 64, count = (KT - wave + W - 1) / W;  // this wave's blocks: wave, wave + W, ...
+
+  PA pa;
+  PB pb;
+  pa.by_rows(g.a + (long long)t.m0 * g.lda, g.lda, (t.rows - 1) * (int)g.lda + 2 * g.k, g.k, 0, lane,
+             [](int r) { return r; });
+  if constexpr (B_COL)
+    pb.by_columns(g.b + t.group * g.b_group + 2 * t.n0, g.ldb, g.k, g.n - t.n0, 0, lane);
+  else
+    pb.by_rows(g.b + t.group * g.b_group, g.ldb, (GATED ? 2 : 1) * g.n * (int)g.ldb, g.k, 0, lane, [&](int r) {
+      return GATED && r >= BN ? g.n + min(t.n0 + r - BN, g.n - 1) : min(t.n0 + r, g.n - 1);
+    });
+  auto issue = [&](int i, int slot) {
+    const int kt = wave + i * W;
+#pragma unroll
+    for (int q = 0; q < PA::INS; ++q) pa.issue(q, kt, kt == KT - 1, ring + slot * SLOT, 0);
+#pragma unroll
+    for (int q = 0; q < PB::INS; ++q) pb.issue(q, kt, kt == KT - 1, ring + slot * SLOT + PA::CH, 0);
+  };
+  f32x16_ffn acc[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+#pragma unroll
+  for (int q = 0; q < S; ++q)
+    if (q < count) issue(q, q);
+  int slot = 0;
+  for (int i = 0; i < count; ++i) {
+    wait_rings_lgkm0<NP, 0, S - 1, 0>(count - 1 - i);  // block i has landed
+    const u32x4* at = ring + slot * SLOT;
+    bf16x8_ffn fa[4], fb[4][NB];
+#pragma unroll
+    for (int sub = 0; sub < 4; ++sub) {
+      fa[sub] = PA::read(at, 0, sub, lane);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) fb[sub][j] = PB::read(at + PA::CH, 32 * j, sub, lane);
+    }
+    wait_vmcnt_lgkm0<63>();  // it is in registers: its slot is free
+    if (i + S < count) issue(i + S, slot);
+#pragma unroll
+    for (int sub = 0; sub < 4; ++sub)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[sub][j], fa[sub], acc[j], 0, 0, 0);
+    if (++slot == S) slot = 0;
+  }
+
+  // Each wave's sums to a patch of its own ring; then every thread adds 8 columns of a row.
+  constexpr int PITCH = 32 * NB + 4;
+  static_assert(32 * PITCH * 4 <= S * SLOT * 16, "a patch within the wave's ring");
+  float* patch = reinterpret_cast<float*>(ring);
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<f32x4_ffn*>(patch + (lane & 31) * PITCH + 32 * j + 8 * q + 4 * (lane >> 5)) =
+          f32x4_ffn{acc[j][4 * q], acc[j][4 * q + 1], acc[j][4 * q + 2], acc[j][4 * q + 3]};
+  __syncthreads();
+  constexpr int LPR = BN / 8;
+  using Out = FfnStore<KIND, F32>;
+  for (int at = threadIdx.x; at < t.rows * LPR; at += 64 * W) {
+    const int row = at / LPR, col = at % LPR * 8;
+    if (t.n0 + col >= g.n) continue;
+    typename Out::Old old;
+    Out::load(g, t, g.c, row, t.n0 + col, old);
+    float v[8], up[8];
+    auto take = [&](float (&to)[8], int c) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) to[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const float* from = reinterpret_cast<const float*>(lds + w * (S * SLOT)) + row * PITCH + c;
+        const f32x4_ffn lo = *reinterpret_cast<const f32x4_ffn*>(from), hi = *reinterpret_cast<const f32x4_ffn*>(from + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          to[i] += lo[i];
+          to[4 + i] += hi[i];
+        }
+      }
+    };
+    take(v, col);
+    if constexpr (GATED) take(up, 32 + col);
+    Out::store(g, t, g.c, row, t.n0 + col, old, v, up);
   }
 }
 
