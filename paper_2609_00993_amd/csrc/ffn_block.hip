@@ -61,8 +61,6 @@ __global__ __launch_bounds__(RA == 8 ? 512 : 256) void ffn_block_few(FfnArgs g) 
 
 // ------------------------------------------------------------------ gradients of the weights
 
-constexpr int kFfnWeightRows = 128, kFfnWeightCols = 256;
-
 // Workgroup b's tile: parts of the rows outermost, then groups; within a group blocks of four
 // column tiles, row tile by row tile; runs of consecutive tiles dealt to the XCDs in turn.
 __device__ __forceinline__ bool ffn_weight_tile(const FfnArgs& g, int bm, int bn, FfnTile& t, int& split) {
@@ -102,41 +100,34 @@ __global__ __launch_bounds__(256, 2) void ffn_block_weights(FfnArgs g) {
   ffn_tile<kFfnWeightGrad, F32, kFfnWeightRows, kFfnWeightCols, 32, 2, 2, 3, 3>(g, t, c, lds);
 }
 
-// The parts' sums, in order, to the result.
+// The parts' sums, in order, to the result: four values to a thread, eight parts in flight.
 template <bool F32>
 __global__ __launch_bounds__(256) void ffn_block_join(const float* parts, long long values, int splits, int accumulate,
                                                       uint8_t* out) {
-  const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 8;
+  const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
   if (at >= values) return;
-  float v[8];
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const f32x4_ffn* p = reinterpret_cast<const f32x4_ffn*>(parts + at);
+  f32x4_ffn v = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 8;
+  for (int s = 0; s < splits; s += U) {
+    f32x4_ffn q[U];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = 0.f;
-  for (int s = 0; s < splits; ++s) {
-    const f32x4_ffn* p = reinterpret_cast<const f32x4_ffn*>(parts + s * values + at);
-    const f32x4_ffn lo = p[0], hi = p[1];
+    for (int i = 0; i < U; ++i) q[i] = s + i < splits ? p[(s + i) * (values / 4)] : f32x4_ffn{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] += lo[i];
-      v[4 + i] += hi[i];
-    }
-  }
-  uint8_t* p = out + at * (F32 ? 4 : 2);
-  if (accumulate) {
-    float old[8];
-    if constexpr (F32) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) old[i] = reinterpret_cast<const float*>(p)[i];
-    } else {
-      ffn_unpack8(load16(p), old);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += old[i];
+    for (int i = 0; i < U; ++i) v += q[i];
   }
   if constexpr (F32) {
-    store16(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
-    store16(p + 16, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+    f32x4_ffn* o = reinterpret_cast<f32x4_ffn*>(out + at * 4);
+    *o = accumulate ? *o + v : v;
   } else {
-    store16(p, ffn_bf16x8(v));
+    u32x2* o = reinterpret_cast<u32x2*>(out + at * 2);
+    if (accumulate) {
+      const u32x2 w = *o;
+      v += f32x4_ffn{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16),
+                     __uint_as_float(w[1] & 0xffff0000u)};
+    }
+    *o = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
   }
 }
 
@@ -217,19 +208,8 @@ bool aligned16(const P*... p) {
 
 int size_of(int32_t dtype) { return dtype == MOE_DTYPE_F32 ? 4 : 2; }
 
-// Parts of the rows for the weights' gradient: enough tiles to fill the GPU twice, and at
-// least four slices to a part.  128 x 128 tiles of 64 KB: 512 of them are 2^25 bytes.
-int weight_splits(long long rows, int groups, long long tiles) {
-  const long long slices = rows / groups / 64;
-  long long s = (512 + tiles - 1) / tiles;
-  s = s < slices / 4 ? s : slices / 4;
-  return tiles >= 384 || s < 2 ? 1 : (int)s;
-}
-long long weight_tiles(int groups, int m, int n) { 
-  return (long long)groups * ((m + kFfnWeightRows - 1) / kFfnWeightRows) * ((n + kFfnWeightCols - 1) / kFfnWeightCols);
-}
 long long weight_bytes(long long rows, int groups, int m, int n) {
-  const int s = weight_splits(rows, groups, weight_tiles(groups, m, n));
+  const int s = ffn_weight_parts(rows, groups, m, n);
   return s > 1 ? 4LL * s * groups * m * n : 0;
 }
 bool weight_shape_ok(int64_t rows, int32_t groups, int32_t m, int32_t n) {
@@ -373,7 +353,7 @@ int moe_ffn_weight_grad(const void* a, int64_t a_stride, const void* b, int64_t 
   g.groups = groups;
   g.m = m;
   g.n = n;
-  g.splits = need > 0 ? weight_splits(rows, groups, weight_tiles(groups, m, n)) : 1;
+  g.splits = ffn_weight_parts(rows, groups, m, n);
   g.c = g.splits > 1 ? (uint8_t*)workspace : (uint8_t*)dw;
   g.accumulate = g.splits > 1 ? 0 : accumulate != 0;
   g.ldc = (long long)n * (g.splits > 1 ? 4 : size_of(dw_dtype));
@@ -393,7 +373,7 @@ int moe_ffn_weight_grad(const void* a, int64_t a_stride, const void* b, int64_t 
   if (!launched()) return MOE_ERR_HIP;
   if (g.splits > 1) {
     const long long values = (long long)groups * m * n;
-    const dim3 blocks((unsigned)((values / 8 + 255) / 256));
+    const dim3 blocks((unsigned)((values / 4 + 255) / 256));
     if (f32) ffn_block_join<true><<<blocks, 256, 0, stream>>>((const float*)workspace, values, g.splits, accumulate != 0, (uint8_t*)dw);
     else ffn_block_join<false><<<blocks, 256, 0, stream>>>((const float*)workspace, values, g.splits, accumulate != 0, (uint8_t*)dw);
     if (!launched()) return MOE_ERR_HIP;

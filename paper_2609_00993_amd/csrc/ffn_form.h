@@ -57,4 +57,30 @@ inline FfnForm ffn_form(int kind, long long rows, int groups, int n, int k) {
   return best;
 }
 
+constexpr int kFfnWeightRows = 128, kFfnWeightCols = 256;  // of a tile of the weights' gradients
+constexpr long long kFfnPartBytes = 1LL << 27;            // of the parts' sums, at most
+
+// Parts that a group's rows are cut into, each with float32 sums of its own which a second launch
+// adds: where tiles are few and rows many.  In ns: a slice of 32 rows takes a tile 500 alone on
+// its CU and 830 beside another, the parts' sums 8 bytes a value to write and read at 4500 bytes, a launch 4000.
+// Measured, one group, us: 1000 rows, 2048 x 2048, one part 20, three 38; 16000 rows, 512 x 512, 20 parts 24, 62 parts 66;
+// 16000 rows, 2048 x 2048, two 147, four 137.
+inline int ffn_weight_parts(long long rows, int groups, int m, int n) {
+  const long long tiles = (long long)groups * ((m + kFfnWeightRows - 1) / kFfnWeightRows) *
+                          ((n + kFfnWeightCols - 1) / kFfnWeightCols);
+  const double values = (double)groups * m * n;
+  const long long slices = (rows / groups + 31) / 32;
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= 64 && (s == 1 || (s <= slices / 4 && 4 * s * values <= kFfnPartBytes)); ++s) {
+    const long long wgs = tiles * s;
+    const double rounds = wgs <= kFfnCus ? 500 : 830.0 * ((wgs + 2 * kFfnCus - 1) / (2 * kFfnCus));
+    const double ns = rounds * ((slices + s - 1) / s) + (s > 1 ? 4000 + s * values * 8 / 4500 : 0);
+    if (s > 1 && ns >= least) continue;
+    least = ns;
+    best = s;
+  }
+  return best;
+}
+
 }  // namespace moepd
