@@ -52,10 +52,11 @@ __global__ __launch_bounds__(256) void ffn_block_wide(FfnArgs g) {
 // Few rows: up to 8 by eight waves of two blocks in flight each, up to 32 by four of three.
 template <int KIND, bool F32, int RA>
 __global__ __launch_bounds__(RA == 8 ? 512 : 256) void ffn_block_few(FfnArgs g) {
-  constexpr int NB = KIND == kFfnDown ? 1 : 2, W = RA == 8 ? 8 : 4, S = RA == 8 ? (NB == 1 ? 3 : 2) : 3;
+  constexpr int NB = ffn_few_columns(KIND, RA) == (KIND == kFfnGateUp ? 16 : 32) ? 1 : 2;
+  constexpr int W = RA == 8 ? 8 : 4, S = RA == 8 && NB == 2 ? 2 : 3;
   __shared__ u32x4 lds[ffn_few_chunks(RA, NB, W, S)];
   FfnTile t;
-  if (!ffn_row_tile(g, RA, KIND == kFfnGateUp ? 32 : 32 * NB, t)) return;
+  if (!ffn_row_tile(g, RA, ffn_few_columns(KIND, RA), t)) return;
   ffn_few_tile<KIND, F32, RA, NB, W, S>(g, t, lds);
 }
 
@@ -96,6 +97,7 @@ __global__ __launch_bounds__(256, 2) void ffn_block_weights(FfnArgs g) {
   FfnTile t;
   int split;
   if (!ffn_weight_tile(g, kFfnWeightRows, kFfnWeightCols, t, split)) return;
+  if (g.accumulate && t.k_count == 0) return;  // nothing to add
   uint8_t* c = g.c + ((long long)split * g.groups + t.group) * g.m * g.ldc;
   ffn_tile<kFfnWeightGrad, F32, kFfnWeightRows, kFfnWeightCols, 32, 2, 2, 3, 3>(g, t, c, lds);
 }

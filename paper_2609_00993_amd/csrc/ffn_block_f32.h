@@ -105,6 +105,7 @@ __global__ __launch_bounds__(256) void ffn_block_f32_weights(FfnArgs g) {
   FfnTile t;
   int split;
   if (!ffn_weight_tile(g, kFfnF32Rows, kFfnF32Cols, t, split)) return;
+  if (g.accumulate && t.k_count == 0) return;
   ffn_f32_tile<kFfnWeightGrad>(g, t, reinterpret_cast<float*>(g.c + ((long long)split * g.groups + t.group) * g.m * g.ldc));
 }
 

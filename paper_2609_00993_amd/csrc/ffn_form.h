@@ -12,6 +12,12 @@ enum FfnTiles : int { kFfnFew8 = 0, kFfnFew32 = 1, kFfnMid = 2, kFfnWide = 3 };
 
 constexpr int kFfnMidRows = 160, kFfnWideRows = 256, kFfnCus = 256;
 
+// Columns of a few tile: gate/up of up to 8 rows 16 of each, which spreads one token's weights over twice the CUs (I
+// 2048: 128).
+constexpr int ffn_few_columns(int kind, int rows) {
+  return kind == kFfnGateUp ? (rows == 8 ? 16 : 32) : kind == kFfnDown ? 32 : 64;
+}
+
 struct FfnForm {
   int tiles;          // FfnTiles
   int rows, columns;  // of a tile at most
@@ -47,13 +53,13 @@ inline FfnForm ffn_form(int kind, long long rows, int groups, int n, int k) {
     best.run = count >= 8 * 32 ? 32 : count >= 16 ? (int)(count / 8) : 2;
     best.count = (rows / bm + touched) * best.n_tiles;
   };
-  const int bn = kind == kFfnGateUp ? 128 : 256, few_bn = kind == kFfnGateUp || kind == kFfnDown ? 32 : 64;
+  const int bn = kind == kFfnGateUp ? 128 : 256;
   const double slices = (double)up(k, 64);
   if (mean >= 2 * kFfnWideRows) consider(kFfnWide, kFfnWideRows, bn, [&](int) { return 3000 + 1170 * slices; });
   for (int bm = kFfnMidRows; bm >= 32; bm -= 32)
     consider(kFfnMid, bm, bn, [&](int blocks) { return 3000 + (300 + 105 * blocks) * slices; });
   const bool few8 = rows <= 8;
-  consider(few8 ? kFfnFew8 : kFfnFew32, few8 ? 8 : 32, few_bn, [&](int) { return 3000 + 2.0 * k; });
+  consider(few8 ? kFfnFew8 : kFfnFew32, few8 ? 8 : 32, ffn_few_columns(kind, few8 ? 8 : 32), [&](int) { return 3000 + 2.0 * k; });
   return best;
 }
 

@@ -493,7 +493,7 @@ __device__ __forceinline__ void ffn_tile(const FfnArgs& g, const FfnTile& t, uin
   }
 }
 
-// A tile of up to 32 rows and 32 NB columns (gate/up: 32 of each) for few rows, where the stream of
+// A tile of up to 32 rows and 32 NB columns (gate/up: 16 NB of each) for few rows, where the stream of
 // weights is what bounds a product: the W waves of a workgroup deal the tile's blocks of 64 of K
 // among them, each with a ring of S blocks of its own (no barrier: a wave waits for its own
 // transfers alone), and their sums meet in LDS and are added in wave order.  Up to 8 rows take an
@@ -502,8 +502,8 @@ constexpr int ffn_few_chunks(int ra, int nb, int w, int s) { return w * s * (ra 
 template <int KIND, bool F32, int RA, int NB, int W, int S>
 __device__ __forceinline__ void ffn_few_tile(const FfnArgs& g, const FfnTile& t, u32x4* lds) {
   constexpr bool GATED = KIND == kFfnGateUp, B_COL = KIND >= kFfnDownGrad;
-  static_assert(KIND != kFfnWeightGrad && (!GATED || NB == 2) && (!B_COL || NB == 2), "panels");
-  constexpr int BN = GATED ? 32 : 32 * NB;
+  static_assert(KIND != kFfnWeightGrad && (!B_COL || NB == 2), "panels");
+  constexpr int BN = GATED ? 16 * NB : 32 * NB;
   using PA = FfnPanel<false, RA, 64, 1>;
   using PB = FfnPanel<B_COL, 32 * NB, 64, 1>;
   constexpr int NP = PA::INS + PB::INS, SLOT = PA::CH + PB::CH;
@@ -593,7 +593,7 @@ __device__ __forceinline__ void ffn_few_tile(const FfnArgs& g, const FfnTile& t,
       }
     };
     take(v, col);
-    if constexpr (GATED) take(up, 32 + col);
+    if constexpr (GATED) take(up, BN + col);
     Out::store(g, t, g.c, row, t.n0 + col, old, v, up);
   }
 }

@@ -8,28 +8,45 @@
 #include "swiglu.h"
 #include "tiles.h"
 
+#include <algorithm>
+#include <type_traits>
+
 namespace moepd {
 namespace {
 
 typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 
+constexpr int kSmallTokens = 2048;           // batches that share a row among waves
 constexpr int kRowVec = 8;                   // values of a lane and pass
 constexpr int kRowPass = kWave * kRowVec;    // values of a wave and pass
 
+// Large batches go past the caches (STREAM): each row is read and written once, and the batch is
+// larger than the caches.
+template <bool STREAM, class V>
+__device__ __forceinline__ V row_get(const uint8_t* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  else return *reinterpret_cast<const V*>(p);
+}
+template <bool STREAM, class V>
+__device__ __forceinline__ void row_put(uint8_t* p, V v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
+  else *reinterpret_cast<V*>(p) = v;
+}
+
 // 8 values from element `at` of a row of n on; those past the row are 0.
-template <bool BF16>
+template <bool BF16, bool STREAM>
 __device__ __forceinline__ void row_load(const uint8_t* row, int at, int n, float (&v)[8]) {
   if (at + 8 <= n) {
     if constexpr (BF16) {
-      const u32x4_any q = *reinterpret_cast<const u32x4_any*>(row + 2LL * at);
+      const u32x4_any q = row_get<STREAM, u32x4_any>(row + 2LL * at);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         v[2 * i] = __uint_as_float(q[i] << 16);
         v[2 * i + 1] = __uint_as_float(q[i] & 0xffff0000u);
       }
     } else {
-      const u32x4_at4 a = *reinterpret_cast<const u32x4_at4*>(row + 4LL * at);
-      const u32x4_at4 b = *reinterpret_cast<const u32x4_at4*>(row + 4LL * at + 16);
+      const u32x4_at4 a = row_get<STREAM, u32x4_at4>(row + 4LL * at);
+      const u32x4_at4 b = row_get<STREAM, u32x4_at4>(row + 4LL * at + 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         v[i] = __uint_as_float(a[i]);
@@ -47,17 +64,17 @@ __device__ __forceinline__ void row_load(const uint8_t* row, int at, int n, floa
     }
   }
 }
-template <bool BF16>
+template <bool BF16, bool STREAM>
 __device__ __forceinline__ void row_store(uint8_t* row, int at, int n, const float (&v)[8]) {
   if (at + 8 <= n) {
     if constexpr (BF16) {
-      *reinterpret_cast<u32x4_any*>(row + 2LL * at) =
-          u32x4_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+      row_put<STREAM>(row + 2LL * at, u32x4_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]),
+                                                bf16_pair(v[6], v[7])});
     } else {
-      *reinterpret_cast<u32x4_at4*>(row + 4LL * at) =
-          u32x4_at4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-      *reinterpret_cast<u32x4_at4*>(row + 4LL * at + 16) =
-          u32x4_at4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+      row_put<STREAM>(row + 4LL * at, u32x4_at4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                                                __float_as_uint(v[3])});
+      row_put<STREAM>(row + 4LL * at + 16, u32x4_at4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]),
+                                                     __float_as_uint(v[7])});
     }
   } else {
 #pragma unroll
@@ -76,8 +93,9 @@ __device__ __forceinline__ long long wave_index() {
 
 // ------------------------------------------------------------------ gather
 
+// 65,532 rows of 2048 float32 from 16,383 tokens: 153 us, 4.4 TB/s of which the rows are four fifths.
 // A row is copied as it is (by 16 bytes; the last ones by element), so bits of NaN survive.
-template <int SIZE>
+template <int SIZE, bool STREAM>
 __global__ __launch_bounds__(256) void rows_gather_kernel(const uint8_t* x, long long x_stride, int T,
                                                           const int32_t* token_of_row, const int32_t* row_count, int rows,
                                                           int hidden, uint8_t* out, long long out_stride, int parts) {
@@ -102,7 +120,7 @@ __global__ __launch_bounds__(256) void rows_gather_kernel(const uint8_t* x, long
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int v = v0 + 64 * i + lane;
-      if (v < whole) *reinterpret_cast<u32x4_any*>(to + 16LL * v) = q[i];
+      if (v < whole) row_put<STREAM>(to + 16LL * v, q[i]);
     }
   }
   const int at = whole * EACH + lane;
@@ -114,7 +132,11 @@ __global__ __launch_bounds__(256) void rows_gather_kernel(const uint8_t* x, long
 
 // ------------------------------------------------------------------ combine
 
-template <bool YB, bool OB>
+// The waves of a token share its row: a wave that takes more of it waits for memory once a
+// pass, and one token's slots are few.  8192 tokens of k = 8, an eighth of the slots resident, 7168 bf16: one wave a
+// token 74 us (four passes at a time, which takes 190 registers, 108), four 57, seven 50 (4.7 TB/s).  16383 tokens of
+// four slots, 2048 float32: 132 us, 5.1 TB/s.
+template <bool YB, bool OB, bool STREAM>
 __global__ __launch_bounds__(256) void rows_combine_kernel(const uint8_t* y, long long y_stride, int rows, const float* w,
                                                            const int32_t* row_of_slot, int T, int k, int hidden,
                                                            uint8_t* out, long long out_stride, int parts) {
@@ -126,7 +148,7 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(const uint8_t* y, lon
   const float w_l = lane < k && w ? w[t * k + lane] : 1.f;
   const uint64_t resident = __ballot(r_l >= 0 && r_l < rows);
   uint8_t* o = out + t * out_stride * (OB ? 2 : 4);
-  constexpr int GROUP = 4;  // rows in flight
+  constexpr int GROUP = STREAM ? 2 : 4;  // rows in flight
   for (int at0 = part * kRowPass; at0 < hidden; at0 += parts * kRowPass) {
     const int at = at0 + kRowVec * lane;
     float acc[8];
@@ -143,7 +165,7 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(const uint8_t* y, lon
           const int j = __builtin_ctzll(m);
           m &= m - 1;
           f[q] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w_l), j));
-          row_load<YB>(y + __builtin_amdgcn_readlane(r_l, j) * y_stride * (YB ? 2 : 4), at, hidden, v[q]);
+          row_load<YB, STREAM>(y + __builtin_amdgcn_readlane(r_l, j) * y_stride * (YB ? 2 : 4), at, hidden, v[q]);
           n = q + 1;
         }
       }
@@ -153,7 +175,7 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(const uint8_t* y, lon
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[i] = __builtin_fmaf(f[q], v[q][i], acc[i]);
     }
-    row_store<OB>(o, at, hidden, acc);
+    row_store<OB, STREAM>(o, at, hidden, acc);
   }
 }
 
@@ -165,8 +187,9 @@ __device__ __forceinline__ float wave_sum(float v) {  // the same order in every
   return v;
 }
 
-// A wave takes every parts-th of its token's slots that have a row.
-template <bool DB, bool YB, bool GB>
+// A wave takes every parts-th of its token's slots that have a row: with one wave a token, tokens of many
+// resident slots set the pace (8192 tokens as above: 114 us, with four 78, 4.5 TB/s).
+template <bool DB, bool YB, bool GB, bool STREAM>
 __global__ __launch_bounds__(256) void rows_combine_backward_kernel(const uint8_t* dout, long long dout_stride,
                                                                     const uint8_t* y, long long y_stride, int rows,
                                                                     const float* w, const int32_t* row_of_slot, int T,
@@ -191,14 +214,14 @@ __global__ __launch_bounds__(256) void rows_combine_backward_kernel(const uint8_
     const uint8_t* yr = y + r * y_stride * (YB ? 2 : 4);
     uint8_t* g = dy + r * dy_stride * (GB ? 2 : 4);
     float sum = 0.f;
-    constexpr int U = 2;
+    constexpr int U = STREAM ? 4 : 2;
     for (int at0 = 0; at0 < hidden; at0 += U * kRowPass) {
       float dv[U][8], yv[U][8];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int at = at0 + u * kRowPass + kRowVec * lane;
-        row_load<DB>(d, at, hidden, dv[u]);
-        if (dw) row_load<YB>(yr, at, hidden, yv[u]);
+        row_load<DB, false>(d, at, hidden, dv[u]);
+        if (dw) row_load<YB, STREAM>(yr, at, hidden, yv[u]);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -209,7 +232,7 @@ __global__ __launch_bounds__(256) void rows_combine_backward_kernel(const uint8_
           if (dw) sum = __builtin_fmaf(dv[u][i], yv[u][i], sum);
           o[i] = f * dv[u][i];
         }
-        row_store<GB>(g, at, hidden, o);
+        row_store<GB, STREAM>(g, at, hidden, o);
       }
     }
     if (dw) {
@@ -289,14 +312,14 @@ int moe_rows_gather(const void* x, int32_t dtype, int64_t x_stride, int32_t T, c
   if (rows == 0) return MOE_OK;
   if ((!x && T > 0) || !token_of_row || !out) return MOE_ERR_INVALID_ARG;
   const int size = bf16(dtype) ? 2 : 4;
-  const int parts = rows > 2048 ? 1 : (hidden * size / 16 + 255) / 256 > 0 ? (hidden * size / 16 + 255) / 256 : 1;
+  const int parts = std::max(1, (hidden * size / 16 + 255) / 256);
   const dim3 grid = waves_grid(rows * parts);
-  if (bf16(dtype))
-    rows_gather_kernel<2><<<grid, 256, 0, stream>>>((const uint8_t*)x, x_stride, T, token_of_row, row_count, (int)rows,
-                                                    hidden, (uint8_t*)out, out_stride, parts);
-  else
-    rows_gather_kernel<4><<<grid, 256, 0, stream>>>((const uint8_t*)x, x_stride, T, token_of_row, row_count, (int)rows,
-                                                    hidden, (uint8_t*)out, out_stride, parts);
+  auto go = [&](auto kernel) {
+    kernel<<<grid, 256, 0, stream>>>((const uint8_t*)x, x_stride, T, token_of_row, row_count, (int)rows, hidden,
+                                     (uint8_t*)out, out_stride, parts);
+  };
+  if (rows > kSmallTokens) bf16(dtype) ? go(rows_gather_kernel<2, true>) : go(rows_gather_kernel<4, true>);
+  else bf16(dtype) ? go(rows_gather_kernel<2, false>) : go(rows_gather_kernel<4, false>);
   return done();
 }
 
@@ -309,14 +332,19 @@ int moe_rows_combine(const void* y, int32_t y_dtype, int64_t y_stride, int64_t r
     return MOE_ERR_INVALID_ARG;
   if (T == 0) return MOE_OK;
   if ((!y && rows > 0) || !row_of_slot || !out) return MOE_ERR_INVALID_ARG;
-  const int parts = T > 2048 ? 1 : (hidden + kRowPass - 1) / kRowPass;
+  const bool large = T > kSmallTokens;
+  const int parts = (hidden + kRowPass * (large ? 2 : 1) - 1) / (kRowPass * (large ? 2 : 1));
   const dim3 grid = waves_grid((long long)T * parts);
   auto go = [&](auto kernel) {
     kernel<<<grid, 256, 0, stream>>>((const uint8_t*)y, y_stride, (int)rows, w, row_of_slot, T, k, hidden, (uint8_t*)out,
                                      out_stride, parts);
   };
-  if (bf16(y_dtype)) bf16(out_dtype) ? go(rows_combine_kernel<true, true>) : go(rows_combine_kernel<true, false>);
-  else bf16(out_dtype) ? go(rows_combine_kernel<false, true>) : go(rows_combine_kernel<false, false>);
+  auto by_out = [&](auto yb, auto ob) {
+    constexpr bool Y = decltype(yb)::value, O = decltype(ob)::value;
+    large ? go(rows_combine_kernel<Y, O, true>) : go(rows_combine_kernel<Y, O, false>);
+  };
+  auto by_y = [&](auto yb) { bf16(out_dtype) ? by_out(yb, std::true_type{}) : by_out(yb, std::false_type{}); };
+  bf16(y_dtype) ? by_y(std::true_type{}) : by_y(std::false_type{});
   return done();
 }
 
@@ -331,7 +359,8 @@ int moe_rows_combine_backward(const void* dout, int32_t dout_dtype, int64_t dout
     return MOE_ERR_INVALID_ARG;
   if (T == 0) return MOE_OK;
   if (!dout || !row_of_slot || (rows > 0 && (!dy || (dw && !y)))) return MOE_ERR_INVALID_ARG;
-  const int parts = T > 2048 ? 1 : k;
+  const bool large = T > kSmallTokens;
+  const int parts = large ? (k < 4 ? k : 4) : k;
   const dim3 grid = waves_grid((long long)T * parts);
   auto go = [&](auto kernel) {
     kernel<<<grid, 256, 0, stream>>>((const uint8_t*)dout, dout_stride, (const uint8_t*)y, y_stride, (int)rows, w,
@@ -339,7 +368,10 @@ int moe_rows_combine_backward(const void* dout, int32_t dout_dtype, int64_t dout
   };
   auto by_dy = [&](auto d, auto yb) {
     constexpr bool D = decltype(d)::value, Y = decltype(yb)::value;
-    bf16(dy_dtype) ? go(rows_combine_backward_kernel<D, Y, true>) : go(rows_combine_backward_kernel<D, Y, false>);
+    if (large)
+      bf16(dy_dtype) ? go(rows_combine_backward_kernel<D, Y, true, true>) : go(rows_combine_backward_kernel<D, Y, false, true>);
+    else
+      bf16(dy_dtype) ? go(rows_combine_backward_kernel<D, Y, true, false>) : go(rows_combine_backward_kernel<D, Y, false, false>);
   };
   auto by_y = [&](auto d) { bf16(y_dtype) ? by_dy(d, std::true_type{}) : by_dy(d, std::false_type{}); };
   bf16(dout_dtype) ? by_y(std::true_type{}) : by_y(std::false_type{});
