@@ -1,0 +1,38 @@
+"""Registers, LDS and spills of the built kernels of the feed-forward block, the token rows and AdamW (no GPU):
+what their launches count on."""
+
+from tests.kernel_resources import VGPR_UNIT, VGPRS_PER_LANE, kernels, resources
+
+LDS = 160 * 1024
+MINE = ("ffn_block", "rows_", "adamw_")
+
+
+def test_no_kernel_spills():
+    got = {n: r for n, r in resources().items() if n.startswith(MINE)}
+    # products: six of mid, wide and of each few height; weights' gradients and their join by type; float32: four and weights'
+    assert sum(n.startswith("ffn_block") for n in got) == 6 * 4 + 2 + 2 + 5, sorted(got)
+    # gather by size, combine by two types, its gradient by three, each plain and past the caches; the gate's by type
+    assert sum(n.startswith("rows_") for n in got) == 4 + 8 + 16 + 2, sorted(got)
+    assert sum(n.startswith("adamw_") for n in got) == 4, sorted(got)
+    for name, r in got.items():
+        assert (r["vgpr_spill_count"], r["sgpr_spill_count"], r["private_segment_fixed_size"]) == (0, 0, 0), name
+
+
+def test_ring_tiles_fit_a_cu():
+    for name, (vgprs, lds) in kernels().items():
+        if name.startswith(("ffn_block_mid", "ffn_block_wide", "ffn_block_few")):
+            waves = 2 if name.startswith("ffn_block_few") and name.endswith(", 8>") else 1  # to a SIMD
+            assert lds <= LDS and vgprs * waves <= VGPRS_PER_LANE, (name, vgprs, lds)
+
+
+def test_two_weight_tiles_share_a_cu():
+    got = {n: v for n, v in kernels().items() if n.startswith("ffn_block_weights")}
+    assert len(got) == 2
+    for name, (vgprs, lds) in got.items():
+        assert 2 * lds <= LDS and 2 * vgprs <= VGPRS_PER_LANE, (name, vgprs, lds)
+
+
+def test_row_kernels_leave_room_for_four_waves_to_a_simd():
+    for name, (vgprs, lds) in kernels().items():
+        if name.startswith(("rows_", "adamw_")):
+            assert vgprs <= VGPRS_PER_LANE // 4 // VGPR_UNIT * VGPR_UNIT and lds == 0, (name, vgprs, lds)
