@@ -91,7 +91,8 @@ __device__ __forceinline__ bool ffn_weight_tile(const FfnArgs& g, int bm, int bn
   return true;
 }
 
-template <bool F32>
+// ADD: bf16 results that are added to what is there.
+template <bool F32, bool ADD>
 __global__ __launch_bounds__(256, 2) void ffn_block_weights(FfnArgs g) {
   __shared__ u32x4 lds[ffn_chunks(kFfnWeightRows, kFfnWeightCols, 32, 3, 3)];
   FfnTile t;
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(256, 2) void ffn_block_weights(FfnArgs g) {
   if (!ffn_weight_tile(g, kFfnWeightRows, kFfnWeightCols, t, split)) return;
   if (g.accumulate && t.k_count == 0) return;  // nothing to add
   uint8_t* c = g.c + ((long long)split * g.groups + t.group) * g.m * g.ldc;
-  ffn_tile<kFfnWeightGrad, F32, kFfnWeightRows, kFfnWeightCols, 32, 2, 2, 3, 3>(g, t, c, lds);
+  ffn_tile<kFfnWeightGrad, F32, kFfnWeightRows, kFfnWeightCols, 32, 2, 2, 3, 3, !F32 && !ADD>(g, t, c, lds);
 }
 
 // The parts' sums, in order, to the result: four values to a thread, eight parts in flight.
@@ -370,8 +371,9 @@ int moe_ffn_weight_grad(const void* a, int64_t a_stride, const void* b, int64_t 
   if (tiles > kMostBlocks) return MOE_ERR_INVALID_ARG;
   const dim3 grid = grid_of((tiles + 7) / 8 * 8, 256);
   if (dtype == MOE_DTYPE_F32) ffn_block_f32_weights<<<grid, 256, 0, stream>>>(g);
-  else if (f32 || g.splits > 1) ffn_block_weights<true><<<grid, 256, 0, stream>>>(g);
-  else ffn_block_weights<false><<<grid, 256, 0, stream>>>(g);
+  else if (f32 || g.splits > 1) ffn_block_weights<true, false><<<grid, 256, 0, stream>>>(g);
+  else if (accumulate) ffn_block_weights<false, true><<<grid, 256, 0, stream>>>(g);
+  else ffn_block_weights<false, false><<<grid, 256, 0, stream>>>(g);
   if (!launched()) return MOE_ERR_HIP;
   if (g.splits > 1) {
     const long long values = (long long)groups * m * n;

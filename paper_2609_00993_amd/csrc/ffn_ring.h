@@ -257,7 +257,8 @@ struct FfnStore {
 constexpr int ffn_chunks(int bm, int br, int bk, int sa, int sb) { return (sa * bm + sb * br) * (bk / 8); }
 
 // A tile of BM rows and BR columns (gate/up: BR / 2 of each), by a WM x WN grid of waves.
-template <int KIND, bool F32, int BM, int BR, int BK, int WM, int WN, int SA, int SB>
+template <int KIND, bool F32, int BM, int BR, int BK, int WM, int WN, int SA, int SB,
+          bool HALF = !F32 && KIND != kFfnGateUp && KIND != kFfnDownGrad>
 __device__ __forceinline__ void ffn_tile(const FfnArgs& g, const FfnTile& t, uint8_t* c, u32x4* lds) {
   constexpr bool GATED = KIND == kFfnGateUp, A_COL = KIND == kFfnWeightGrad, B_COL = KIND >= kFfnDownGrad;
   constexpr int NB = GATED ? 2 : 1, BN = BR / NB;
@@ -450,46 +451,72 @@ __device__ __forceinline__ void ffn_tile(const FfnArgs& g, const FfnTile& t, uin
   // Results go out through LDS, 32 rows of the wave's columns at a time (within a wave LDS
   // operations complete in order): written as the accumulators lie, rows 16 bytes apart
   // beyond their width, read back 8 columns of a row to a lane, so that memory sees whole
-  // lines and the elementwise part works on 16-byte vectors.
-  constexpr int PITCH = WTN + 4, PATCH = 32 * PITCH;  // floats
-  static_assert(4 * NB * PATCH <= 4 * ffn_chunks(BM, BR, BK, SA, SB), "patches within the ring");
-  float* patch = reinterpret_cast<float*>(lds) + wave * (NB * PATCH);
+  // lines.  Where nothing else is done to them they are rounded on the way in (HALF), which
+  // halves what passes through LDS: it, not the MFMAs, bounds the weights' gradients of short groups (257
+  // rows, 4096 x 7168 of 32 groups: 675 us without, 625 with).
   constexpr int LPR = WTN / 8, RPP = 64 / LPR, PASSES = 32 / RPP;
-  using Out = FfnStore<KIND, F32>;
   const int rr0 = lane / LPR, col = lane % LPR * 8, n_at = t.n0 + wn * WTN + col;
+  if constexpr (HALF) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    constexpr int PITCH = WTN * 2 + 16, PATCH = 32 * PITCH;  // bytes
+    static_assert(4 * PATCH <= 16 * ffn_chunks(BM, BR, BK, SA, SB) && !GATED, "patches within the ring");
+    uint8_t* patch = reinterpret_cast<uint8_t*>(lds) + wave * PATCH;
 #pragma unroll
-  for (int fm = 0; fm < FM; ++fm) {
-    typename Out::Old old[PASSES];
-    const int row0 = wm * WTM + fm * 32;
+    for (int fm = 0; fm < FM; ++fm) {
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      const int row = row0 + p * RPP + rr0;
-      if (row < t.rows && n_at < g.n) Out::load(g, t, c, row, n_at, old[p]);
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<u32x2*>(patch + (lane & 31) * PITCH + 2 * (j * 32 + 8 * q + 4 * (lane >> 5))) =
+              u32x2{bf16_pair(acc[fm][j][4 * q], acc[fm][j][4 * q + 1]), bf16_pair(acc[fm][j][4 * q + 2], acc[fm][j][4 * q + 3])};
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        const int rr = p * RPP + rr0, row = wm * WTM + fm * 32 + rr;
+        const u32x4 v = load16(patch + rr * PITCH + 2 * col);
+        if (row < t.rows && n_at < g.n) ffn_store16(c + (long long)(t.m0 + row) * g.ldc + 2 * n_at, v);
+      }
+      __builtin_amdgcn_wave_barrier();
     }
+  } else {
+    constexpr int PITCH = WTN + 4, PATCH = 32 * PITCH;  // floats; gate/up: one of each
+    static_assert(4 * NB * PATCH <= 4 * ffn_chunks(BM, BR, BK, SA, SB), "patches within the ring");
+    float* patch = reinterpret_cast<float*>(lds) + wave * (NB * PATCH);
+    using Out = FfnStore<KIND, F32>;
 #pragma unroll
-    for (int j = 0; j < FB; ++j)
+    for (int fm = 0; fm < FM; ++fm) {
+      typename Out::Old old[PASSES];
+      const int row0 = wm * WTM + fm * 32;
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4_ffn*>(patch + j / FN * PATCH + (lane & 31) * PITCH + j % FN * 32 + 8 * q + 4 * (lane >> 5)) =
-            f32x4_ffn{acc[fm][j][4 * q], acc[fm][j][4 * q + 1], acc[fm][j][4 * q + 2], acc[fm][j][4 * q + 3]};
-    __builtin_amdgcn_wave_barrier();
+      for (int p = 0; p < PASSES; ++p) {
+        const int row = row0 + p * RPP + rr0;
+        if (row < t.rows && n_at < g.n) Out::load(g, t, c, row, n_at, old[p]);
+      }
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      const int rr = p * RPP + rr0, row = row0 + rr;
-      float v[8], up[8];
-      auto take = [&](float (&to)[8], const float* from) {
-        const f32x4_ffn lo = *reinterpret_cast<const f32x4_ffn*>(from), hi = *reinterpret_cast<const f32x4_ffn*>(from + 4);
+      for (int j = 0; j < FB; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          to[i] = lo[i];
-          to[4 + i] = hi[i];
-        }
-      };
-      take(v, patch + rr * PITCH + col);
-      if constexpr (GATED) take(up, patch + PATCH + rr * PITCH + col);
-      if (row < t.rows && n_at < g.n) Out::store(g, t, c, row, n_at, old[p], v, up);
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<f32x4_ffn*>(patch + j / FN * PATCH + (lane & 31) * PITCH + j % FN * 32 + 8 * q + 4 * (lane >> 5)) =
+              f32x4_ffn{acc[fm][j][4 * q], acc[fm][j][4 * q + 1], acc[fm][j][4 * q + 2], acc[fm][j][4 * q + 3]};
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        const int rr = p * RPP + rr0, row = row0 + rr;
+        float v[8], up[8];
+        auto take = [&](float (&to)[8], const float* from) {
+          const f32x4_ffn lo = *reinterpret_cast<const f32x4_ffn*>(from), hi = *reinterpret_cast<const f32x4_ffn*>(from + 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            to[i] = lo[i];
+            to[4 + i] = hi[i];
+          }
+        };
+        take(v, patch + rr * PITCH + col);
+        if constexpr (GATED) take(up, patch + PATCH + rr * PITCH + col);
+        if (row < t.rows && n_at < g.n) Out::store(g, t, c, row, n_at, old[p], v, up);
+      }
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();
   }
 }
 
