@@ -15,9 +15,10 @@ namespace {
 
 // ------------------------------------------------------------------ rows times a group's weights
 
+template <int SHARE>
 __device__ __forceinline__ bool ffn_row_tile(const FfnArgs& g, int bm, int bn, FfnTile& t) {
   GroupTile w;
-  if (!group_tile<false, true>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), bm, w)) return false;
+  if (!group_tile<false, SHARE>(g, (int)(blockIdx.y * gridDim.x + blockIdx.x), bm, w)) return false;
   t.group = w.group;
   t.m0 = w.m0;
   t.rows = w.m_end - w.m0;
@@ -26,12 +27,10 @@ __device__ __forceinline__ bool ffn_row_tile(const FfnArgs& g, int bm, int bn, F
   return true;
 }
 
-// Tiles cut to the 32-row blocks that they hold; four waves side by side along the columns.
+// A tile of up to 160 rows, cut to the 32-row blocks that it holds; four waves side by side along the
+// columns.
 template <int KIND, bool F32>
-__global__ __launch_bounds__(256) void ffn_block_mid(FfnArgs g) {
-  __shared__ u32x4 lds[ffn_chunks(kFfnMidRows, 256, 64, 3, 3)];
-  FfnTile t;
-  if (!ffn_row_tile(g, g.bm, KIND == kFfnGateUp ? 128 : 256, t)) return;
+__device__ __forceinline__ void ffn_mid_tile(const FfnArgs& g, const FfnTile& t, u32x4* lds) {
   const int blocks = (t.rows + 31) / 32;
   if (blocks <= 1) ffn_tile<KIND, F32, 32, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
   else if (blocks == 2) ffn_tile<KIND, F32, 64, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
@@ -39,14 +38,23 @@ __global__ __launch_bounds__(256) void ffn_block_mid(FfnArgs g) {
   else if (blocks == 4) ffn_tile<KIND, F32, 128, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
   else ffn_tile<KIND, F32, 160, 256, 64, 1, 4, 3, 3>(g, t, g.c, lds);
 }
+template <int KIND, bool F32>
+__global__ __launch_bounds__(256) void ffn_block_mid(FfnArgs g) {
+  __shared__ u32x4 lds[ffn_chunks(kFfnMidRows, 256, 64, 3, 3)];
+  FfnTile t;
+  if (ffn_row_tile(g, g.bm, KIND == kFfnGateUp ? 128 : 256, t)) ffn_mid_tile<KIND, F32>(g, t, lds);
+}
 
-// Groups of many rows: 256 rows, a 2 x 2 grid of waves, the rows' slices one ahead of the weights'.
+// Groups of more rows: tiles of 256 by a 2 x 2 grid of waves, the rows' slices one ahead of the weights', and a
+// rest of up to 160 rows in a tile cut to it.
 template <int KIND, bool F32>
 __global__ __launch_bounds__(256) void ffn_block_wide(FfnArgs g) {
   __shared__ u32x4 lds[ffn_chunks(kFfnWideRows, 256, 64, 3, 2)];
+  static_assert(ffn_chunks(kFfnMidRows, 256, 64, 3, 3) <= ffn_chunks(kFfnWideRows, 256, 64, 3, 2), "the rest's ring");
   FfnTile t;
-  if (!ffn_row_tile(g, kFfnWideRows, KIND == kFfnGateUp ? 128 : 256, t)) return;
-  ffn_tile<KIND, F32, 256, 256, 64, 2, 2, 3, 2>(g, t, g.c, lds);
+  if (!ffn_row_tile<kRowsFull>(g, kFfnWideRows, KIND == kFfnGateUp ? 128 : 256, t)) return;
+  if (t.rows > kFfnMidRows) ffn_tile<KIND, F32, 256, 256, 64, 2, 2, 3, 2>(g, t, g.c, lds);
+  else ffn_mid_tile<KIND, F32>(g, t, lds);
 }
 
 // Few rows: up to 8 by eight waves of two blocks in flight each, up to 32 by four of three.

@@ -11,6 +11,7 @@ namespace {
 
 constexpr int kFfnF32Rows = 64, kFfnF32Cols = 64, kFfnF32Depth = 16;
 
+template <int SHARE = kRowsInBlocks>
 __device__ __forceinline__ bool ffn_row_tile(const FfnArgs& g, int bm, int bn, FfnTile& t);
 __device__ __forceinline__ bool ffn_weight_tile(const FfnArgs& g, int bm, int bn, FfnTile& t, int& split);
 

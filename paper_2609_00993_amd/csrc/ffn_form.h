@@ -27,6 +27,14 @@ struct FfnForm {
   int threads() const { return tiles == kFfnFew8 ? 512 : 256; }
 };
 
+// Whether groups of `mean` rows, of which some have a few more or less, suit wide tiles: not around a
+// full tile and a small rest, where tiles of 160 rows share the rows better.  32 groups, H 7168, I 2048, gate/up and down,
+// us, mid / wide: 200 rows 501 / 428 and 256 / 244; 257 559 / 558 and 291 / 294 (drawn lengths: 527 / 579 and 300 / 269);
+// 300 597 / 614 and 316 / 322; 400 812 / 777 and 428 / 385; 550 1086 / 1024 and 553 / 514.
+constexpr bool ffn_wide_fits(int mean) {
+  return (mean > kFfnMidRows && mean <= kFfnWideRows - 24) || mean >= kFfnWideRows + 96;
+}
+
 // rows in `groups` groups, n columns, K values to a sum.  The times behind the rule, in ns with every CU at work:
 // a slice of 64 of K takes a mid tile 300 + 105 for each 32-row block, a wide one 1170, a few tile's start and
 // join 3000 and each value of K 2; mid and wide tiles start and end in 3000.  Measured, one group, us, mid / few: 128 rows, H
@@ -55,7 +63,15 @@ inline FfnForm ffn_form(int kind, long long rows, int groups, int n, int k) {
   };
   const int bn = kind == kFfnGateUp ? 128 : 256;
   const double slices = (double)up(k, 64);
-  if (mean >= 2 * kFfnWideRows) consider(kFfnWide, kFfnWideRows, bn, [&](int) { return 3000 + 1170 * slices; });
+  if (ffn_wide_fits(mean)) {
+    // full tiles, and a rest of its own height or, a small one, half and half with a full one
+    const int full = mean / kFfnWideRows, rest = (int)up(mean % kFfnWideRows, 32);
+    auto mid_ns = [](int blocks) { return blocks ? 300.0 + 105 * blocks : 0; };
+    const double ns = rest > kFfnMidRows / 32 ? 1170.0 * (full + 1)
+                      : rest <= 2 && rest && full ? 1170.0 * (full - 1) + mid_ns((9 + rest) / 2) + mid_ns((8 + rest) / 2)
+                                                  : 1170.0 * full + mid_ns(rest);
+    consider(kFfnWide, kFfnWideRows, bn, [&](int) { return 3000 + ns / (full + (rest ? 1 : 0)) * slices; });
+  }
   for (int bm = kFfnMidRows; bm >= 32; bm -= 32)
     consider(kFfnMid, bm, bn, [&](int blocks) { return 3000 + (300 + 105 * blocks) * slices; });
   const bool few8 = rows <= 8;

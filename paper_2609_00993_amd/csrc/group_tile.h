@@ -33,6 +33,9 @@ __device__ __forceinline__ int wave_scan(int v) {
   return dpp_plus<0x143, 0xC>(v);  // row_bcast:31
 }
 
+// How a group's rows are shared among its row tiles.
+enum RowShare : int { kRowsEven = 0, kRowsInBlocks = 1, kRowsFull = 2 };
+
 // The tile of workgroup b, if any, found by each wave from the offsets: lane i
 // holds group i's rows, and a scan of the groups' counts of row tiles (of at most bm
 // rows) places the tile; with more than 64 groups, 64 at a time.
@@ -42,8 +45,9 @@ __device__ __forceinline__ int wave_scan(int v) {
 // XCD b % 8, so the row tiles that read one weight panel share an L2, and every XCD
 // streams an eighth of every group's weights.
 //
-// Otherwise (ring tiles): a group's rows are shared evenly among its row tiles (BLOCKS: its
-// blocks of 32 rows are, for tiles cut to them); its
+// Otherwise (ring tiles): a group's rows are shared evenly among its row tiles (kRowsInBlocks: its
+// blocks of 32 rows are, for tiles cut to them; kRowsFull: full tiles and a rest,
+// of which a small one takes half of the last full tile's with it); its
 // tiles run over blocks of four column tiles, in each row tile by row tile; and runs of
 // consecutive tiles are dealt to the XCDs in turn, so that an XCD's L2 serves each row
 // block to four workgroups and each weight panel to as many as the run has row
@@ -51,7 +55,7 @@ __device__ __forceinline__ int wave_scan(int v) {
 // (16 row x 4 column tiles: what an XCD's CUs hold at a time) for groups of many rows,
 // else 32, which leave less to the last round: 96,889 skewed rows (7168 x 2048)
 // 1030 us with 64, 1096 with 32; 32,768 rows 391 / 430; 8192 rows, 256 to a group, 77 / 73.
-template <bool STRIPED, bool BLOCKS = false, class G>
+template <bool STRIPED, int SHARE = kRowsEven, class G>
 __device__ __forceinline__ bool group_tile(const G& g, int b, int bm, GroupTile& t) {
   const int lane = lane_id();
   int l = 0, h = 0, mt = 0, incl = 0;  // of group g0 + lane
@@ -107,7 +111,12 @@ __device__ __forceinline__ bool group_tile(const G& g, int b, int bm, GroupTile&
     const int width = min(4, g.n_tiles - 4 * q);
     const int mi = r / width;
     t.nt = uniform(4 * q + r - mi * width);
-    if constexpr (BLOCKS) {
+    if constexpr (SHARE == kRowsFull) {
+      const int full = bm / 32, rest = (hi - lo + 31) / 32 - full * (mt_e - 1);  // of the last tile, in blocks
+      const int last = rest <= full / 4 && mt_e > 1 ? full * (mt_e - 2) + (full + rest + 1) / 2 : full * (mt_e - 1);
+      t.m0 = uniform(lo + 32 * (mi < mt_e - 1 ? full * mi : last));
+      t.m_end = uniform(min(lo + 32 * (mi + 1 < mt_e - 1 ? full * (mi + 1) : mi + 1 == mt_e - 1 ? last : full * mt_e), hi));
+    } else if constexpr (SHARE == kRowsInBlocks) {
       const int nb = (hi - lo + 31) / 32;
       t.m0 = uniform(lo + (int)((long long)nb * mi / mt_e) * 32);
       t.m_end = uniform(min(lo + (int)((long long)nb * (mi + 1) / mt_e) * 32, hi));

@@ -46,6 +46,7 @@ CASES = {
     # 256 rows, one to six slices, groups of one row beside large ones
     "wide-1": (6000, 64, 2312),
     "wide-3": ([0, 2500, 2501, 6000], 136, 2312),
+    "wide-halves": ([0, 2600, 5161, 5420, 6000], 136, 2312),  # rests of one and two blocks, shared with a full tile
     "wide-6": (6001, 328, 2312),
     "wide-2-3": (6000, 2312, 72),
     "wide-4-7": ([7, 3000, 5999], 2312, 200),
