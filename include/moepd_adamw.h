@@ -61,7 +61,8 @@ typedef struct moe_adamw moe_adamw_t;
 
 /* The table of `count` tensors (1 to 65536) on the current device, with states of
  * state_bits (32 or 8).  The buffers are borrowed: they stay where they are for the table's
- * lifetime, and none may overlap another.  Waits for the table's copy.  Errors:
+ * lifetime, and none may overlap another.  Waits for the table's copy; not for use while a
+ * stream captures.  Errors:
  * MOE_ERR_INVALID_ARG, MOE_ERR_OOM, MOE_ERR_HIP; *out is then NULL and nothing is left
  * allocated. */
 int moe_adamw_create(const moe_adamw_tensor_t* tensors, int32_t count, int32_t state_bits, moe_adamw_t** out);

@@ -32,8 +32,8 @@
  * Strides are in elements, multiples of 8, at least the row's width and at most
  * 2^20, or 0 for exactly that; pointers are 16-byte aligned.  w_gate_up: [groups,
  * 2I, H], w_down: [groups, H, I].  No buffer that is written may overlap another
- * argument, but h may be NULL in moe_ffn_down_backward and gate_up in
- * moe_ffn_gate_up.
+ * argument.  A launch of more than 2^31 - 2^16 workgroups (one for each tile of at
+ * least 32 rows and 32 columns) is refused with MOE_ERR_INVALID_ARG.
  *
  * Conventions: as in moepd.h (status codes, borrowed device pointers, host
  * validation before anything is enqueued, no allocation, no synchronisation, a

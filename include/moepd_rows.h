@@ -24,7 +24,8 @@
  * order, results in bf16 rounded once.  T in [0, 2^24], k in [1, 16], hidden in
  * [1, 2^20], rows in [0, 2^31 - 512].  Types are MOE_DTYPE_F32 or MOE_DTYPE_BF16.
  * Strides are in elements, at least the row's width, or 0 for exactly that;
- * pointers need their element's alignment.
+ * pointers need their element's alignment.  No buffer that is written may overlap
+ * another argument.
  */
 #ifndef MOEPD_ROWS_H
 #define MOEPD_ROWS_H

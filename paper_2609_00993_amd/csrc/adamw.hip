@@ -5,7 +5,7 @@
 #include <math.h>
 #include <string.h>
 
-#include <new>
+#include <memory>
 #include <vector>
 
 #include "common.h"
@@ -339,7 +339,7 @@ int moe_adamw_create(const moe_adamw_tensor_t* tensors, int32_t count, int32_t s
       if (chunks > (1LL << 31) - (1 << 16)) return MOE_ERR_INVALID_ARG;
       of.insert(of.end(), (size_t)here, i);
     }
-    moe_adamw* h = new moe_adamw;
+    std::unique_ptr<moe_adamw> h(new moe_adamw);
     h->bits = state_bits;
     h->chunks = chunks;
     h->runs = runs;
@@ -355,12 +355,11 @@ int moe_adamw_create(const moe_adamw_tensor_t* tensors, int32_t count, int32_t s
     if (st != MOE_OK) {
       (void)hipGetLastError();
       if (h->mem) (void)hipFree(h->mem);
-      delete h;
       return st;
     }
     h->tensors = static_cast<const AdamTensor*>(h->mem);
     h->tensor_of = reinterpret_cast<const int32_t*>(static_cast<uint8_t*>(h->mem) + table);
-    *out = h;
+    *out = h.release();
     return MOE_OK;
   } catch (...) {
     return MOE_ERR_OOM;
