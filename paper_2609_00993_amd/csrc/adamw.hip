@@ -1,7 +1,8 @@
 // An AdamW step over many tensors, with states in 32 bits or in blocks of 8 (include/moepd_adamw.h).
 // One launch: the table lists every chunk's tensor, a workgroup takes one chunk.  What bounds
 // it is memory: 28 bytes an element with 32-bit states beside bf16 weights and float32
-// masters, 16.1 with 8-bit states.
+// masters, 16.1 with 8-bit states.  201 million elements: 1086 us and 620, 5.2 TB/s both (a copy: 5.03); with nontemporal
+// accesses 1180 and 652.
 #include <math.h>
 #include <string.h>
 
@@ -323,7 +324,7 @@ int moe_adamw_create(const moe_adamw_tensor_t* tensors, int32_t count, int32_t s
       return MOE_ERR_INVALID_ARG;
     total += (t.n + kAdamRun - 1) / kAdamRun;
   }
-  // Chunks of four passes where there are enough of them to fill the GPU several times over.
+  // Chunks of four passes where these still fill the GPU several times over (at most 16 workgroups a CU without).
   const int runs = total >= 4 * 4096 ? kAdamRuns : 1;
   try {
     std::vector<AdamTensor> host((size_t)count);

@@ -28,7 +28,8 @@ __device__ __forceinline__ bool ffn_row_tile(const FfnArgs& g, int bm, int bn, F
 }
 
 // A tile of up to 160 rows, cut to the 32-row blocks that it holds; four waves side by side along the
-// columns.
+// columns.  32 groups, H 7168, I 2048, gate/up: 128 rows each 350 us, the weights at 5.7 TB/s; 320 rows 571, 1050
+// TFLOP/s.  Two workgroups to a CU with 32-deep slices, whose rows are half a line, were 22 % slower at 257 rows.
 template <int KIND, bool F32>
 __device__ __forceinline__ void ffn_mid_tile(const FfnArgs& g, const FfnTile& t, u32x4* lds) {
   const int blocks = (t.rows + 31) / 32;
@@ -45,7 +46,7 @@ __global__ __launch_bounds__(256) void ffn_block_mid(FfnArgs g) {
   if (ffn_row_tile(g, g.bm, KIND == kFfnGateUp ? 128 : 256, t)) ffn_mid_tile<KIND, F32>(g, t, lds);
 }
 
-// Groups of more rows: tiles of 256 by a 2 x 2 grid of waves, the rows' slices one ahead of the weights', and a
+// Groups of more rows (1024 in each of 32 groups, H 7168, I 2048: gate/up 1494 us, 1290 TFLOP/s): tiles of 256 by a 2 x 2 grid of waves, the rows' slices one ahead of the weights', and a
 // rest of up to 160 rows in a tile cut to it.
 template <int KIND, bool F32>
 __global__ __launch_bounds__(256) void ffn_block_wide(FfnArgs g) {
@@ -57,7 +58,8 @@ __global__ __launch_bounds__(256) void ffn_block_wide(FfnArgs g) {
   else ffn_mid_tile<KIND, F32>(g, t, lds);
 }
 
-// Few rows: up to 8 by eight waves of two blocks in flight each, up to 32 by four of three.
+// Few rows: up to 8 by eight waves of two or three blocks in flight each, up to 32 by four of three.  One token, H
+// 7168, I 2048: gate/up 12 us (4.7 TB/s of weights), down 7; 256 rows: gate/up 37, where a tile of 160 rows takes 81.
 template <int KIND, bool F32, int RA>
 __global__ __launch_bounds__(RA == 8 ? 512 : 256) void ffn_block_few(FfnArgs g) {
   constexpr int NB = ffn_few_columns(KIND, RA) == (KIND == kFfnGateUp ? 16 : 32) ? 1 : 2;
@@ -99,6 +101,10 @@ __device__ __forceinline__ bool ffn_weight_tile(const FfnArgs& g, int bm, int bn
   return true;
 }
 
+// Two workgroups share a CU.  What bounds them, for the few hundred rows of a group in training, is the results'
+// way out, through LDS and to memory: w_gate_up's gradient of 32 groups, 4096 x 7168, 128 rows 405 us (4.9 TB/s), 257
+// 610, 512 1050 (920 TFLOP/s); results past the caches 883 -> 717 at 257 rows, rounded before LDS 675 -> 625.  256 x 128
+// tiles are 3 % slower (their rows of results are half as long), 128 x 128, three to a CU, 5.
 // ADD: bf16 results that are added to what is there.
 template <bool F32, bool ADD>
 __global__ __launch_bounds__(256, 2) void ffn_block_weights(FfnArgs g) {
