@@ -324,7 +324,7 @@ int moe_adamw_create(const moe_adamw_tensor_t* tensors, int32_t count, int32_t s
       return MOE_ERR_INVALID_ARG;
     total += (t.n + kAdamRun - 1) / kAdamRun;
   }
-  // Chunks of four passes where these still fill the GPU several times over (at most 16 workgroups a CU without).
+  // Chunks of four passes where these still make 16 workgroups a CU.
   const int runs = total >= 4 * 4096 ? kAdamRuns : 1;
   try {
     std::vector<AdamTensor> host((size_t)count);

@@ -183,8 +183,8 @@ __device__ __forceinline__ void ffn_store16(uint8_t* p, const u32x4& v) {
   __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
 }
 
-// What 8 neighbouring results of one row become.  Where(row) gives places, load() what
-// has to be read before (issued ahead of the staging), store() the rest.
+// What 8 neighbouring results of one row become: load() what has to be read for them (issued ahead of
+// their way through LDS), store() the rest.
 template <int KIND, bool F32>
 struct FfnStore {
   struct Old {

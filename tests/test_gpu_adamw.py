@@ -185,6 +185,16 @@ def test_zeros_and_small(bits):
         x.check(i, **how)
 
 
+def test_smallest_scales():
+    """m near and below the smallest normal float32: scale byte 0, and codes in steps of 2^-136."""
+    rng = np.random.default_rng(9)
+    ts = [One(rng, 64, 8, grad="f32", size=s) for s in (1e-36, 1e-37, 1e-38, 3e-39)]
+    how = _step(ts, 8)
+    for i, x in enumerate(ts):
+        x.check(i, **how)
+    assert (ts[2].ms == 0).all() and (ts[2].m != 0).any()
+
+
 def test_states_that_are_not_finite():
     """A NaN or an infinity makes its block's codes NaN, and no other's."""
     import torch
