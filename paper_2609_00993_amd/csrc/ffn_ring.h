@@ -568,6 +568,7 @@ __device__ __forceinline__ void ffn_few_tile(const FfnArgs& g, const FfnTile& t,
   int slot = 0;
   for (int i = 0; i < count; ++i) {
     wait_rings_lgkm0<NP, 0, S - 1, 0>(count - 1 - i);  // block i has landed
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);           // the reads stay behind the wait
     const u32x4* at = ring + slot * SLOT;
     bf16x8_ffn fa[4], fb[4][NB];
 #pragma unroll
@@ -577,6 +578,7 @@ __device__ __forceinline__ void ffn_few_tile(const FfnArgs& g, const FfnTile& t,
       for (int j = 0; j < NB; ++j) fb[sub][j] = PB::read(at + PA::CH, 32 * j, sub, lane);
     }
     wait_vmcnt_lgkm0<63>();  // it is in registers: its slot is free
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
     if (i + S < count) issue(i + S, slot);
 #pragma unroll
     for (int sub = 0; sub < 4; ++sub)
