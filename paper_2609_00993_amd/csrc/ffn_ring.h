@@ -577,7 +577,8 @@ __device__ __forceinline__ void ffn_few_tile(const FfnArgs& g, const FfnTile& t,
 #pragma unroll
       for (int j = 0; j < NB; ++j) fb[sub][j] = PB::read(at + PA::CH, 32 * j, sub, lane);
     }
-    wait_vmcnt_lgkm0<63>();  // it is in registers: its slot is free
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);  // and ahead of the next
+    wait_vmcnt_lgkm0<63>();                   // it is in registers: its slot is free
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     if (i + S < count) issue(i + S, slot);
 #pragma unroll

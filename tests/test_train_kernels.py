@@ -1,7 +1,14 @@
 """Registers, LDS and spills of the built kernels of the feed-forward block, the token rows and AdamW (no GPU):
 what their launches count on."""
 
-from tests.kernel_resources import VGPR_UNIT, VGPRS_PER_LANE, kernels, resources
+import os
+import re
+import subprocess
+import tempfile
+
+from tests.kernel_resources import READELF, VGPR_UNIT, VGPRS_PER_LANE, _code_objects, kernels, resources
+
+OBJDUMP = os.path.join(os.path.dirname(READELF), "llvm-objdump")
 
 LDS = 160 * 1024
 MINE = ("ffn_block", "rows_", "adamw_")
@@ -36,3 +43,38 @@ def test_row_kernels_leave_room_for_four_waves_to_a_simd():
     for name, (vgprs, lds) in kernels().items():
         if name.startswith(("rows_", "adamw_")):
             assert vgprs <= VGPRS_PER_LANE // 4 // VGPR_UNIT * VGPR_UNIT and lds == 0, (name, vgprs, lds)
+
+
+def _listings(prefix):
+    """{kernel: its instructions as built} of the gfx950 code objects in the library."""
+    got = {}
+    for elf in _code_objects():
+        with tempfile.NamedTemporaryFile(suffix=".co") as f:
+            f.write(elf)
+            f.flush()
+            text = subprocess.run([OBJDUMP, "-d", "--no-show-raw-insn", f.name], stdout=subprocess.PIPE, text=True, check=True).stdout
+        for name, body in re.findall(r"^[0-9a-f]+ <(\w+)>:\n(.*?)(?=^[0-9a-f]+ <|\Z)", text, re.M | re.S):
+            if prefix in name:
+                got[name] = [line.split("//")[0].strip() for line in body.split("\n") if line.strip()]
+    return got
+
+
+def test_few_tiles_read_a_slot_before_it_is_filled_again():
+    """A wave's own ring has no barrier: each block's LDS reads are waited for before the next transfer into LDS is
+    issued, and come after the wait for the transfers of their block."""
+    got = _listings("ffn_block_few")
+    assert len(got) == 12
+    for name, lines in got.items():
+        reading, landed, transfers = False, False, 0
+        for line in lines:
+            if line.startswith("ds_read"):
+                assert landed, (name, line)
+                reading = True
+            elif line.startswith("s_waitcnt"):
+                reading = reading and "lgkmcnt(0)" not in line
+                landed = landed or "vmcnt" in line
+            elif line.startswith("buffer_load") and line.endswith("lds"):
+                assert not reading, (name, line)
+                transfers += 1
+                landed = False
+        assert transfers > 0, name
