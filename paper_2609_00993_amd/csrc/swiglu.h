@@ -26,21 +26,30 @@ __device__ __forceinline__ float swiglu_of(float g, float u) {
 }
 
 // From dh to the gradients in gate and up: dg = dh u s (1 + g (1 - s)), du = dh g s, with s =
-// 1 / (1 + e^-g) from q = e^-|g|, which never overflows.  g q is 0 from where q is, infinite
-// gates included.
+// 1 / (1 + e^-g) and q as in swiglu_of (the compiler computes it once for both).  g q is 0 from where
+// q is, infinite gates included.  Of deep gates s, as q, carries a factor of 2^64, which u or dh gives
+// back: good down to gates of -131.  The slope meets the larger of u and dh first, and the
+// factor goes from the smaller one if that is above 1, else from the larger: nothing on the
+// way to a normal dg passes below the normal numbers, or (factors above 5e36 aside) past the range.
 __device__ __forceinline__ void swiglu_grad(float g, float u, float dh, float& dg, float& du) {
 #pragma clang fp contract(off)
   constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
-  const float a = __builtin_fabsf(g) > 256.f ? 256.f : __builtin_fabsf(g);  // NaN stays
+  const float a = fminf(__builtin_fabsf(g), 256.f);
   const float t = -a * kLog2e;
-  const float lo = __builtin_fmaf(-a, kLog2eLow, __builtin_fmaf(-a, kLog2e, -t));  // see swiglu_of
-  const float e = __builtin_amdgcn_exp2f(t);
+  const float lo = __builtin_fmaf(-a, kLog2eLow, __builtin_fmaf(-a, kLog2e, -t));
+  const bool deep = g < -44.f;
+  const float k = deep ? 0x1p-64f : 1.f;
+  const float e = __builtin_amdgcn_exp2f(t + (deep ? 64.f : 0.f));
   const float q = __builtin_fmaf(e, lo * kLn2, e);
-  const float near = __builtin_amdgcn_rcpf(1.f + q), far = q * near;  // s and 1 - s where g >= 0
+  const float near = __builtin_amdgcn_rcpf(__builtin_fmaf(q, k, 1.f)), far = q * near;  // s and 1 - s where g >= 0
   const float s = g < 0.f ? far : near;
-  const float rest = a * (g < 0.f ? -near : far);  // g (1 - s)
-  dg = dh * u * s * (1.f + rest);
-  du = dh * ((g < 0.f ? -a : g) * s);
+  const float m = g < 0.f ? -a : g;
+  const float slope = s * (1.f + (g > 256.f ? 0.f : m * (g < 0.f ? near : far)));  // far is 0 past 256; NaN stays
+  const bool swap = __builtin_fabsf(dh) > __builtin_fabsf(u);
+  const float large = swap ? dh : u, small = swap ? u : dh;
+  const bool above = __builtin_fabsf(small) > 1.f;
+  dg = large * (above ? 1.f : k) * slope * (small * (above ? k : 1.f));
+  du = m * s * (dh * k);
 }
 
 // Two values to bf16, nearest even, packed.

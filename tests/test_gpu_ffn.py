@@ -449,3 +449,51 @@ def test_rows_past_32_bit_offsets():
         want = A.t() @ xs
         tol = (hi - lo + 8) * 2 * U * (A.abs().t() @ xs.abs()) + 2.0 ** -24 * want.abs()
         assert ((dw[e].double() - want).abs() <= tol).all(), e
+
+
+def _activation(dtype, g, u, dh):
+    """(dg, du, h anew) of moe_ffn_down_backward for gates, ups and dh (w_down is the identity), and those three as the type
+    holds them; g, u, dh: [rows, 8]."""
+    import torch
+
+    from paper_2609_00993_amd import moepd as M
+
+    rows, I = g.shape
+    d_gu, d_dy = _dev(np.concatenate([g, u], axis=1), dtype), _dev(dh, dtype)
+    w = _dev(np.eye(8)[None], dtype)
+    d, h = (torch.full((rows, n), SENTINEL, dtype=_torch_type(dtype), device="cuda") for n in (2 * I, I))
+    torch.cuda.synchronize()
+    M.check(M.moe_ffn_down_backward(d_dy, 0, rows, w, d_gu, 1, None, 8, I, _code(dtype), d, h, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    d, gu = _host(d), _host(d_gu)
+    return (d[:, :I], d[:, I:], _host(h)), (gu[:, :I], gu[:, I:], _host(d_dy))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_slope_of_far_gates(dtype):
+    """Gates whose e^-|g| is below the normal numbers, beside ups and dh that bring the results back, and ups and dh whose
+    product alone passes the range: relative errors. q is within 4 u (2^x and its argument 2 u, a fused product 2 u), the reciprocal
+    2 u, 1 + g (1 - s) 4 u (it does not cancel below -2), the products 3 u: 16 u, beside the type's rounding; results below the
+    normal numbers 2^-126."""
+    g, u, dh = np.meshgrid([-20.0, -44.0, -45.0, -49.0, -49.25, -60.0, -80.0, -87.0, -88.0, -92.0, -100.0, -104.0, -120.0, -130.0,
+                            3.0, 50.0], [2.0, -1e10, 1e30, 3e-5], [0.5, -1e-5, 3e7, 1e-30])
+    g, u, dh = (a.reshape(-1, 8) for a in (g, u, dh))
+    (dg, du, h), (g, u, dh) = _activation(dtype, g, u, dh)
+    want_g, want_u = F.swiglu_gradient(g, u, dh)
+    for got, want in ((dg, want_g), (du, want_u), (h, F.swiglu(g, u))):
+        assert (np.abs(want) < 1e38).all() and (np.abs(want) > 1e-30).sum() > want.size // 3
+        assert (np.abs(got - want) <= (16 * U + _step(dtype)) * np.abs(want) + 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_slope_of_large_factors(dtype):
+    """dh u past the range where the slope brings the result back, 0 among the slopes."""
+    g = np.array([[-300.0, -1e30, -132.0, -100.0, -90.0, -60.0, -49.0, -30.0]])
+    u, dh = np.full((1, 8), 1e25), np.full((1, 8), 2e20)
+    (dg, du, _), (g, u, dh) = _activation(dtype, g, u, dh)
+    want_g, want_u = F.swiglu_gradient(np.maximum(g, -256), u, dh)
+    for got, want in ((dg, want_g), (du, want_u)):
+        want = np.where(g < -131, 0.0, want)  # the slope is 0 there
+        inside = np.abs(want) < 3e38
+        assert inside.sum() >= 7 and (np.abs(got - want) <= (16 * U + _step(dtype)) * np.abs(want) + 2.0 ** -126)[inside].all()
+        assert (np.abs(got[~inside]) >= 3e38).all()
