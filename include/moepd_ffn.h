@@ -17,7 +17,8 @@
  * Rows of a matrix lie side by side; gate_up and dgate_up are [rows, 2I], gate
  * (dg) in the columns [0, I) and up (du) in [I, 2I).  Products and sums are
  * float32.  Results in bf16 are rounded once, to nearest even; h and dgate_up, the
- * operands of the products that follow, are such results.
+ * operands of the products that follow, are such results.  A gate of minus infinity takes
+ * the limits (h, dg and du are 0 where u and dh are finite), one of plus infinity too (s is 1, dg = dh u).
  *
  * Arguments that the calls share:
  *   rows     [0, 2^31 - 512]; sizes the launch

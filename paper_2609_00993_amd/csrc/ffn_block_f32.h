@@ -78,7 +78,7 @@ __device__ __forceinline__ void ffn_f32_tile(const FfnArgs& g, const FfnTile& t,
           c[row * 2 * g.n + col] = v;
           c[row * 2 * g.n + g.n + col] = up;
         }
-        reinterpret_cast<float*>(g.h)[row * g.n + col] = swiglu_of(v, up);
+        reinterpret_cast<float*>(g.h)[row * g.n + col] = swiglu_of<true>(v, up);
       } else if constexpr (KIND == kFfnDownGrad) {
         const float* gu = reinterpret_cast<const float*>(g.gu) + row * 2 * g.n + col;
         const float gate = gu[0], up = gu[g.n];
@@ -86,7 +86,7 @@ __device__ __forceinline__ void ffn_f32_tile(const FfnArgs& g, const FfnTile& t,
         swiglu_grad(gate, up, v, dg, du);
         c[row * 2 * g.n + col] = dg;
         c[row * 2 * g.n + g.n + col] = du;
-        if (g.h) reinterpret_cast<float*>(g.h)[row * g.n + col] = swiglu_of(gate, up);
+        if (g.h) reinterpret_cast<float*>(g.h)[row * g.n + col] = swiglu_of<true>(gate, up);
       } else {
         float* p = c + row * ldc + col;
         *p = KIND == kFfnWeightGrad && g.accumulate ? *p + v : v;

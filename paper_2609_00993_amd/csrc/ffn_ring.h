@@ -213,7 +213,7 @@ struct FfnStore {
         store16(p + 2 * g.n, ffn_bf16x8(up));
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = swiglu_of(v[i], up[i]);
+      for (int i = 0; i < 8; ++i) v[i] = swiglu_of<true>(v[i], up[i]);
       store16(g.h + r * 2 * g.n + 2 * col, ffn_bf16x8(v));
     } else if constexpr (KIND == kFfnDownGrad) {
       float gate[8], u[8], du[8], h[8];
@@ -221,7 +221,7 @@ struct FfnStore {
       ffn_unpack8(o.q[1], u);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        h[i] = swiglu_of(gate[i], u[i]);
+        h[i] = swiglu_of<true>(gate[i], u[i]);
         swiglu_grad(gate[i], u[i], v[i], v[i], du[i]);
       }
       uint8_t* p = c + r * 4 * g.n + 2 * col;

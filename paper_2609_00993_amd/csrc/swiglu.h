@@ -12,6 +12,8 @@ namespace moepd {
 // below the normal numbers (which the hardware's 2^x flushes), at -87 and -92, while u may
 // bring the result back: there q carries a factor of 2^64 that 1 + q leaves out and u gives
 // back, good down to gates of -131.  Past 256 q is 0 in any case.
+// LIMIT: 0 also for a gate of minus infinity, where g q is NaN.
+template <bool LIMIT = false>
 __device__ __forceinline__ float swiglu_of(float g, float u) {
 #pragma clang fp contract(off)  // t + 64 must start from the rounded t, whose error lo holds
   constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
@@ -22,12 +24,12 @@ __device__ __forceinline__ float swiglu_of(float g, float u) {
   const float k = deep ? 0x1p-64f : 1.f;
   const float e = __builtin_amdgcn_exp2f(t + (deep ? 64.f : 0.f));
   const float q = __builtin_fmaf(e, lo * kLn2, e);
-  return (g < 0.f ? g * q : g) * __builtin_amdgcn_rcpf(__builtin_fmaf(q, k, 1.f)) * (u * k);
+  return (g < 0.f ? (LIMIT ? -a : g) * q : g) * __builtin_amdgcn_rcpf(__builtin_fmaf(q, k, 1.f)) * (u * k);
 }
 
 // From dh to the gradients in gate and up: dg = dh u s (1 + g (1 - s)), du = dh g s, with s =
 // 1 / (1 + e^-g) and q as in swiglu_of (the compiler computes it once for both).  g q is 0 from where
-// q is, infinite gates included.  Of deep gates s, as q, carries a factor of 2^64, which u or dh gives
+// q is.  Of deep gates s, as q, carries a factor of 2^64, which u or dh gives
 // back: good down to gates of -131.  The slope meets the larger of u and dh first, and the
 // factor goes from the smaller one if that is above 1, else from the larger: nothing on the
 // way to a normal dg passes below the normal numbers, or (factors above 5e36 aside) past the range.

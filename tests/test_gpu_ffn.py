@@ -497,3 +497,34 @@ def test_slope_of_large_factors(dtype):
         inside = np.abs(want) < 3e38
         assert inside.sum() >= 7 and (np.abs(got - want) <= (16 * U + _step(dtype)) * np.abs(want) + 2.0 ** -126)[inside].all()
         assert (np.abs(got[~inside]) >= 3e38).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinite_gates_take_the_limits(dtype):
+    """In the forward pass (where a sum passes the range), anew, and in the gradients."""
+    import torch
+
+    from paper_2609_00993_amd import moepd as M
+
+    inf = np.inf
+    g = np.array([[-inf, inf, -inf, inf, -300.0, -3e38, 2.0, -inf]])
+    u, dh = np.array([[3.0, 3.0, -1e30, -0.5, 7.0, -1.0, 4.0, 0.0]]), np.array([[1.0, 2.0, -1e5, 4.0, 1.0, 1e20, 0.5, 0.0]])
+    (dg, du, h), _ = _activation(dtype, g, u, dh)
+    gone = g[0] < -256
+    for got in (dg, du, h):
+        assert (got[0, gone] == 0).all()
+    top = g[0] == inf
+    assert (dg[0, top] == [6.0, -2.0]).all() and (du[0, top] == inf).all() and (h[0, top] == [inf, -inf]).all()
+    assert not np.isnan(dg).any() and not np.isnan(du).any() and not np.isnan(h).any()
+
+    x = np.array([[1e38, 2.0, 0, 0, 0, 0, 0, 0]])  # the gate's sum is 1e38 of the first column's weight, up 2
+    w = np.zeros((1, 16, 8))
+    w[0, :8, 0], w[0, 8:, 1] = [-100.0, 100.0, -1e38, 1.0, 0.0, -1e-38, -1.0, 1e38], 1.0
+    out, gu = (torch.full((1, n), SENTINEL, dtype=_torch_type(dtype), device="cuda") for n in (8, 16))
+    d_x, d_w = _dev(x, dtype), _dev(w, dtype)
+    torch.cuda.synchronize()
+    M.check(M.moe_ffn_gate_up(d_x, 0, 1, d_w, 1, None, 8, 8, _code(dtype), gu, out, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    gate, h = _host(gu)[0, :8], _host(out)[0]
+    assert (gate[[0, 2]] == -inf).all() and (gate[[1, 7]] == inf).all() and (_host(gu)[0, 8:] == 2).all()
+    assert (h[[0, 2, 4, 6]] == 0).all() and (h[[1, 7]] == inf).all() and not np.isnan(h).any()
