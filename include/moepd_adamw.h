@@ -8,6 +8,9 @@
  *   p = p - lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p)
  * in float32.  p is the master where there is one, and the parameter its rounding;
  * else the parameter itself (which, in bf16, loses updates below half a step of its own).
+ * The root and the quotient hold for every float32 v and eps, those below the normal numbers
+ * included.  What v adds up to below 2^-150 is 0 there: with an eps of 0 such an element divides by
+ * 0, and one whose m and v are both 0 becomes NaN.
  *
  * States in 8 bits: an expert's weights are most of a model's memory, and 32-bit
  * states take four times that of its bf16 weights.  A block of 32 consecutive values

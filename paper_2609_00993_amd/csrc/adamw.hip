@@ -173,6 +173,13 @@ __device__ __forceinline__ uint32_t adam_code(float q, uint32_t r) {
   return q < __uint_as_float((127u + LOW) << 23) ? low : normal;
 }
 
+// The hardware's root (1 ulp), which takes numbers below the normal ones as 0: with a small eps, or
+// none, these are what an update is divided by.
+__device__ __forceinline__ float adam_root(float v) {
+  const bool low = v < 0x1p-126f;
+  return __builtin_amdgcn_sqrtf(v * (low ? 0x1p64f : 1.f)) * (low ? 0x1p-32f : 1.f);
+}
+
 template <bool SMALL>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   const long long chunk = (long long)blockIdx.y * gridDim.x + blockIdx.x;
@@ -219,8 +226,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
     float root[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      root[i] = SMALL ? sqrtf(v[i]) : __builtin_amdgcn_sqrtf(v[i]);
-      const float u = m[i] * i1 * __builtin_amdgcn_rcpf(__builtin_fmaf(root[i], i2, a.eps));
+      root[i] = SMALL ? sqrtf(v[i]) : adam_root(v[i]);
+      // the hardware's reciprocal, too, takes numbers below the normal ones as 0
+      const float d = __builtin_fmaf(root[i], i2, a.eps), k = d < 0x1p-64f ? 0x1p64f : 1.f;
+      const float u = m[i] * i1 * k * __builtin_amdgcn_rcpf(d * k);
       p[i] -= lr * __builtin_fmaf(t.decay, p[i], u);
     }
     if (t.master) adam_store((uint8_t*)t.master, false, at, in, p);
@@ -376,8 +385,9 @@ int moe_adamw_step(moe_adamw_t* h, double beta1, double beta2, double eps, const
   if (hipGetDevice(&device) != hipSuccess) return MOE_ERR_HIP;
   if (device != h->device) return MOE_ERR_INVALID_ARG;
   if (h->chunks == 0) return MOE_OK;
+  const float eps32 = eps > 0 ? fmaxf((float)eps, 0x1p-149f) : 0.f;  // above 0, as eps is: 0 / eps stays 0
   const AdamArgs a{h->tensors, h->tensor_of, h->chunks, h->runs, (float)beta1, (float)(1.0 - beta1), (float)beta2,
-                   (float)(1.0 - beta2), (float)eps, log(beta1), log(beta2), lr, step, grad_scale, seed};
+                   (float)(1.0 - beta2), eps32, log(beta1), log(beta2), lr, step, grad_scale, seed};
   const dim3 grid = grid_of(h->chunks, 256);
   if (h->bits == 8) adamw_kernel<true><<<grid, 256, 0, stream>>>(a);
   else adamw_kernel<false><<<grid, 256, 0, stream>>>(a);

@@ -393,3 +393,35 @@ def test_refused_on_another_table_or_index():
     for k, w in x.parts.items():
         assert (w == x.around[k]).all(), k
     M.check(M.moe_adamw_destroy(h))
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-40, 1e-30])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_smallest_roots(bits, eps):
+    """v from 1e-36 down below the normal numbers, without an eps that hides it. Each of v's three operations (and the square of an
+    8-bit state's root) rounds to steps of 2^-149 there: four halves of one, and half of their share of v in the root."""
+    rng = np.random.default_rng(21)
+    ts = [One(rng, 200, bits, "f32", False, "f32", size=s) for s in (1e-17, 1e-18, 1e-19, 4e-20, 2e-20)]
+    for x in ts:  # no gradient or state near 0, so that v stays above 2^-141
+        x.grad.copy_(x.grad.sign() * x.grad.abs().clamp(min=x.grad.abs().max().item() / 4))
+        x.g0 = _host(x.grad)
+    how = _step(ts, bits, lr=1e-2, eps=eps)
+    for x in ts:
+        p, m, v = A.step(x.p0, x.g0, x.m0, x.v0, how["lr"], how["t"], how["b1"], how["b2"], eps, x.decay, 1.0)
+        assert v.min() > 2.0 ** -141 and (ts[0] is x or v.min() < 2.0 ** -126)
+        c1, c2 = 1 - how["b1"] ** how["t"], 1 - how["b2"] ** how["t"]
+        den = np.sqrt(v / c2) + eps
+        update, slack = np.abs(m) / c1 / den, 4 * U * (how["b1"] * np.abs(x.m0) + np.abs(x.g0)) / c1 / den
+        tol = how["lr"] * ((32 * U + 2.0 ** -148 / v) * update + slack + 4 * U * np.abs(x.decay * x.p0)) + 3 * U * np.abs(p)
+        got = _host(x.param)
+        assert np.isfinite(got).all() and (np.abs(got - p) <= tol).all() and (np.abs(got - x.p0) > 1e-4).any()
+
+
+@pytest.mark.parametrize("eps", [1e-38, 1e-40, 1e-44, 1e-60])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_zeros_over_the_smallest_eps(bits, eps):
+    """Elements that never had a gradient decay, and nothing else."""
+    x = One(np.random.default_rng(22), 100, bits, "f32", False, zeros=True)
+    how = _step([x], bits, lr=0.5, eps=eps)
+    want = x.p0.astype(np.float64) * (1 - how["lr"] * float(np.float32(x.decay)))
+    assert (np.abs(_host(x.param) - want) <= 3 * U * np.abs(x.p0)).all()
