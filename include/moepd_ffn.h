@@ -17,11 +17,14 @@
  * Rows of a matrix lie side by side; gate_up and dgate_up are [rows, 2I], gate
  * (dg) in the columns [0, I) and up (du) in [I, 2I).  Products and sums are
  * float32.  Results in bf16 are rounded once, to nearest even; h and dgate_up, the
- * operands of the products that follow, are such results.  A gate of minus infinity takes
- * the limits (h, dg and du are 0 where u and dh are finite), one of plus infinity too (s is 1, dg = dh u).
+ * operands of the products that follow, are such results.  A gate of
+ * minus infinity takes the limits (h, dg and du are 0 where u and dh are finite), one of
+ * plus infinity too (s is 1, dg = dh u).
  *
  * Arguments that the calls share:
- *   rows     [0, 2^31 - 512]; sizes the launch
+ *   rows     [0, 2^31 - 512]; sizes the launch, and picks the tiles as for groups of
+ *            rows / groups rows (a weight gradient's parts too): room far above the rows
+ *            in use costs the speed of tiles for longer groups, and sums in their order
  *   groups   [1, 1024], and offsets: device [groups + 1] int32, ascending; group
  *            g has the rows [offsets[g], offsets[g + 1]) (values are clamped to [0,
  *            rows]; a dispatch's offsets), which may be none.  Rows of no group

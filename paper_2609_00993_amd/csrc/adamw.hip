@@ -1,7 +1,7 @@
 // An AdamW step over many tensors, with states in 32 bits or in blocks of 8 (include/moepd_adamw.h).
 // One launch: the table lists every chunk's tensor, a workgroup takes one chunk.  What bounds
 // it is memory: 28 bytes an element with 32-bit states beside bf16 weights and float32
-// masters, 16.1 with 8-bit states.  201 million elements: 1086 us and 620, 5.2 TB/s both (a copy: 5.03); with nontemporal
+// masters, 16.1 with 8-bit states.  201 million elements: 1088 us and 624, 5.2 TB/s both (a copy: 5.03); with nontemporal
 // accesses 1180 and 652.
 #include <math.h>
 #include <string.h>

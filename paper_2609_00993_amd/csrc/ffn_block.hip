@@ -28,8 +28,8 @@ __device__ __forceinline__ bool ffn_row_tile(const FfnArgs& g, int bm, int bn, F
 }
 
 // A tile of up to 160 rows, cut to the 32-row blocks that it holds; four waves side by side along the
-// columns.  32 groups, H 7168, I 2048, gate/up: 128 rows each 350 us, the weights at 5.7 TB/s; 320 rows 571, 1050
-// TFLOP/s.  Two workgroups to a CU with 32-deep slices, whose rows are half a line, were 22 % slower at 257 rows.
+// columns.  32 groups, H 7168, I 2048, gate/up: 128 rows each 350 us, 5.7 TB/s (the weights 5.4); 320 rows 571,
+// 1050 TFLOP/s.  Two workgroups to a CU with 32-deep slices, whose rows are half a line, were 22 % slower at 257 rows.
 template <int KIND, bool F32>
 __device__ __forceinline__ void ffn_mid_tile(const FfnArgs& g, const FfnTile& t, u32x4* lds) {
   const int blocks = (t.rows + 31) / 32;
@@ -102,8 +102,9 @@ __device__ __forceinline__ bool ffn_weight_tile(const FfnArgs& g, int bm, int bn
 }
 
 // Two workgroups share a CU.  What bounds them, for the few hundred rows of a group in training, is the results'
-// way out, through LDS and to memory: w_gate_up's gradient of 32 groups, 4096 x 7168, 128 rows 405 us (4.9 TB/s), 257
-// 610, 512 1050 (920 TFLOP/s); results past the caches 883 -> 717 at 257 rows, rounded before LDS 675 -> 625.  256 x 128
+// way out, through LDS and to memory: w_gate_up's gradient of 32 groups, 4096 x 7168, a dozen passes in a row, 128 rows
+// 405 to 425 us (4.7 to 4.9 TB/s), 257 610 to 650 (of drawn lengths, forty passes in a row, 698), 512 1050 (920 TFLOP/s);
+// results past the caches 883 -> 717 at 257 rows, rounded before LDS 675 -> 625.  256 x 128
 // tiles are 3 % slower (their rows of results are half as long), 128 x 128, three to a CU, 5.
 // ADD: bf16 results that are added to what is there.
 template <bool F32, bool ADD>

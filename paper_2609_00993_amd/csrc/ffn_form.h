@@ -30,7 +30,8 @@ struct FfnForm {
 // Whether groups of `mean` rows, of which some have a few more or less, suit wide tiles: not around a
 // full tile and a small rest, where tiles of 160 rows share the rows better.  32 groups, H 7168, I 2048, gate/up and down,
 // us, mid / wide: 200 rows 501 / 428 and 256 / 244; 257 559 / 558 and 291 / 294 (drawn lengths: 527 / 579 and 300 / 269);
-// 300 597 / 614 and 316 / 322; 400 812 / 777 and 428 / 385; 550 1086 / 1024 and 553 / 514.
+// 300 597 / 614 and 316 / 322; 400 812 / 777 and 428 / 385; 550 1086 / 1024 and 553 / 514.  One rule for
+// every kind: down alone would take wide tiles at 257 drawn rows too.
 constexpr bool ffn_wide_fits(int mean) {
   return (mean > kFfnMidRows && mean <= kFfnWideRows - 24) || mean >= kFfnWideRows + 96;
 }
@@ -39,8 +40,9 @@ constexpr bool ffn_wide_fits(int mean) {
 // a slice of 64 of K takes a mid tile 300 + 105 for each 32-row block, a wide one 1170, a few tile's start and
 // join 3000 and each value of K 2; mid and wide tiles start and end in 3000.  Measured, one group, us, mid / few: 128 rows, H
 // 7168, I 2048, gate/up 79 / 20, down 26 / 19; 512 rows, H 2048, I 1024, 46 / 14 and 24 / 14; 1000 rows, H 7168, I 2048,
-// gate/up 131 (wide) / 138, down 43 / 118; 500 rows there, mid tiles of 160 / 96 / 64 rows, 81 / 68 / 57.  32 groups of one
-// row, H 2560, I 768: gate/up 37 / 41.
+// gate/up 131 (wide) / 138, down 43 / 118, and what the rule takes there, mid tiles of 64 and 128 rows, 69 and 33; 500 rows
+// there, mid tiles of 160 / 96 / 64 rows, 81 / 68 / 57 (the rule's, of 32: 52).  32 groups of one row, H 2560, I 768: gate/up
+// 37 / 41.
 inline FfnForm ffn_form(int kind, long long rows, int groups, int n, int k) {
   const long long touched = groups < rows ? groups : rows;  // groups that have a row, if shared evenly
   const int mean = (int)((rows + touched - 1) / touched);
